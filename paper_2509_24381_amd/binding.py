@@ -37,6 +37,12 @@ SCHED_SYMBOLS = (
     "rs_sched_queue_length", "rs_sched_queue_ids", "rs_sched_release_request",
 )
 
+# every symbol include/rserve_attend.h declares
+ATTEND_SYMBOLS = (
+    "rs_rotary_create", "rs_rotary_destroy", "rs_rotary_at", "rs_kv_append", "rs_attend_workspace_bytes", "rs_attend",
+    "rs_kv_attach_bounds", "rs_kv_bounded", "rs_kv_bounds_update", "rs_attend_blocks",
+)
+
 STEPS = ("row_rms", "qkv_gemm", "append_kv", "attention", "o_gemm", "gate_up_gemm", "down_gemm")
 
 
@@ -65,6 +71,12 @@ class _EncodeBatch(C.Structure):
     _fields_ = [("first_segment", C.c_int), ("last_segment", C.c_int), ("n_items", C.c_int), ("n_tokens", C.c_int)]
 
 
+class _RotaryCfg(C.Structure):
+    _fields_ = [("rotary_dim", C.c_int), ("layout", C.c_int), ("max_pos", C.c_int), ("scaling", C.c_int), ("theta", C.c_double),
+                ("factor", C.c_double), ("original_max_pos", C.c_int), ("fast_turns", C.c_double), ("slow_turns", C.c_double),
+                ("magnitude", C.c_double)]
+
+
 class _Weights(C.Structure):
     _fields_ = [("ln1_g", C.c_void_p), ("w_qkv", C.c_void_p), ("b_qkv", C.c_void_p), ("w_o", C.c_void_p),
                 ("ln2_g", C.c_void_p), ("w_gate_up", C.c_void_p), ("w_down", C.c_void_p)]
@@ -86,7 +98,7 @@ def load_library():
     if not os.path.exists(path):
         raise RsError(-5, f"{path} is not built; run `python -m paper_2509_24381_amd.build` (there is no fallback path)")
     lib = C.CDLL(path)
-    vp, sz, i = C.c_void_p, C.c_size_t, C.c_int
+    vp, sz, i, ln = C.c_void_p, C.c_size_t, C.c_int, C.c_long
     proto = {
         "rs_ctx_create": (i, [C.POINTER(_Cfg), C.POINTER(vp)]),
         "rs_ctx_destroy": (None, [vp]),
@@ -133,6 +145,16 @@ def load_library():
         "rs_profile_enable": (i, [vp, i, i]),
         "rs_profile_sample_every": (i, [vp, i]),
         "rs_profile_read": (i, [vp, C.POINTER(C.c_double), C.POINTER(i)]),
+        "rs_rotary_create": (i, [vp, C.POINTER(_RotaryCfg), C.POINTER(vp)]),
+        "rs_rotary_destroy": (None, [vp]),
+        "rs_rotary_at": (i, [vp, i, i, C.POINTER(C.c_float), C.POINTER(C.c_float)]),
+        "rs_kv_append": (i, [vp, vp, i, vp, vp, vp, i, vp, vp, ln, vp, ln, vp, ln, vp, ln, vp]),
+        "rs_attend_workspace_bytes": (sz, [vp, i, i, sz, i]),
+        "rs_attend": (i, [vp, i, vp, vp, i, vp, ln, vp, ln, C.c_float, vp, sz, vp]),
+        "rs_kv_attach_bounds": (i, [vp, vp, vp, i]),
+        "rs_kv_bounded": (i, [vp, i]),
+        "rs_kv_bounds_update": (i, [vp, i, vp, vp, i, vp]),
+        "rs_attend_blocks": (i, [vp, i, vp, vp, i, vp, ln, vp, ln, i, i, i, C.c_float, vp, vp, sz, vp]),
         "rs_sched_create": (i, [i, C.POINTER(vp)]),
         "rs_sched_destroy": (None, [vp]),
         "rs_sched_add_request": (i, [vp, C.c_int64, C.POINTER(_Segment), i]),
@@ -206,6 +228,104 @@ class LayerConfig:
     def _c(self) -> _Cfg:
         return _Cfg(self.hidden, self.n_q_heads, self.n_kv_heads, self.head_dim, self.mlp_inter, self.rms_eps,
                     self.rope_theta, int(self.qkv_bias), self.max_tokens_per_call, self.max_requests, self.max_pos)
+
+
+ROTARY_LAYOUTS = ("halves", "interleaved")
+ROTARY_SCALINGS = ("none", "linear", "ramp", "bands")
+
+
+@dataclass
+class RotaryConfig:
+    """A rotary form (rs_rotary_cfg): the first rotary_dim features of a head in pairs of `layout`, frequencies scaled by `scaling`."""
+    rotary_dim: int
+    theta: float
+    max_pos: int
+    layout: str = "halves"        # or "interleaved"
+    scaling: str = "none"         # or "linear", "ramp", "bands"
+    factor: float = 1.0
+    original_max_pos: int = 0
+    fast_turns: float = 0.0       # 0: 32 (ramp), 4 (bands)
+    slow_turns: float = 0.0       # 0: 1
+    magnitude: float = 0.0        # 0: 1, or 0.1 ln(factor) + 1 (ramp)
+
+    def _c(self) -> _RotaryCfg:
+        for name, names in ((self.layout, ROTARY_LAYOUTS), (self.scaling, ROTARY_SCALINGS)):
+            if name not in names:
+                raise RsError(-1, f"{name!r} is none of {names}")
+        return _RotaryCfg(self.rotary_dim, ROTARY_LAYOUTS.index(self.layout), self.max_pos, ROTARY_SCALINGS.index(self.scaling), self.theta,
+                          self.factor, self.original_max_pos, self.fast_turns, self.slow_turns, self.magnitude)
+
+
+class Rotary:
+    """A rotary form's table of cosines and sines."""
+
+    def __init__(self, ctx: "Context", cfg: RotaryConfig):
+        self.ctx = ctx           # (kept alive as long as the table)
+        self.cfg = cfg
+        self.handle = C.c_void_p()
+        c = cfg._c()
+        _check(ctx.lib.rs_rotary_create(ctx.handle, C.byref(c), C.byref(self.handle)))
+
+    def __del__(self):
+        try:
+            if self.handle:
+                load_library().rs_rotary_destroy(self.handle)
+                self.handle = None
+        except Exception:
+            pass
+
+    def at(self, pos: int, pair: int) -> Tuple[float, float]:
+        """(cos, sin) of one pair at one position, as the table holds them."""
+        c, s = C.c_float(), C.c_float()
+        _check(self.ctx.lib.rs_rotary_at(self.handle, pos, pair, C.byref(c), C.byref(s)))
+        return c.value, s.value
+
+
+def int_array(values):
+    """Whole numbers as the C array that calls take: made once, it spares a serving loop the conversion in every call."""
+    if isinstance(values, C.Array):
+        return values
+    values = [int(v) for v in values]
+    return (C.c_int * max(len(values), 1))(*values)
+
+
+def _ints(values, n: int, what: str):
+    """The address of a C array of at least n whole numbers, or None; the array has to outlive the call."""
+    if values is None:
+        return None
+    a = int_array(values)
+    if len(a) < n or a._type_ is not C.c_int:
+        raise RsError(-1, f"{what} has {len(a)} entries, the call needs {n} ints")
+    return a
+
+
+class CacheSet:
+    """Caches in the order of a call's requests; made once, it spares a serving loop the conversion in every call."""
+
+    def __init__(self, caches: Sequence["KVCache"]):
+        self.caches = list(caches)
+        self.handles = (C.c_void_p * max(len(self.caches), 1))(*[kv.handle.value for kv in self.caches])
+
+    def __len__(self):
+        return len(self.caches)
+
+
+def _cache_set(kvs) -> CacheSet:
+    return kvs if isinstance(kvs, CacheSet) else CacheSet(kvs)
+
+
+def _rows(t, what: str, rows: int, width: int):
+    """(address, distance between rows) of a bf16 tensor [rows, width] or [rows, heads, d] whose rows are contiguous."""
+    import torch
+    shape, stride = t.shape, t.stride()
+    inner = 1
+    for n, s in zip(reversed(shape[1:]), reversed(stride[1:])):
+        if s != inner and n != 1:
+            raise RsError(-1, f"the rows of {what} are not contiguous")
+        inner *= n
+    if t.dtype is not torch.bfloat16 or not shape or shape[0] != rows or inner != width:
+        raise RsError(-1, f"{what} must be bfloat16 [{rows}, {width}]: {t.dtype} {list(shape)}")
+    return t.data_ptr(), stride[0] if rows > 1 else width
 
 
 class PackedWeights:
@@ -303,6 +423,41 @@ class KVCache:
         assert k.is_contiguous() and v.is_contiguous() and k.shape == v.shape
         _check(load_library().rs_kv_import(self.handle, layer, _ptr(k) if n else None, _ptr(v) if n else None, n,
                                            _stream_handle(stream)))
+
+    def attach_bounds(self, codes, units):
+        """Memory for the bounds on this cache's keys (rs_kv_attach_bounds): codes int8 [n_layers, Hkv, blocks, 2, d], units fp32
+        [n_layers, Hkv, blocks], contiguous (with one layer the first dimension may be missing); None, None takes it away."""
+        import torch
+        if codes is not None:
+            cfg = self.ctx.cfg
+            blocks = int(codes.shape[-3])
+            if codes.dtype is not torch.int8 or units.dtype is not torch.float32 or not codes.is_contiguous() or not units.is_contiguous() \
+                    or tuple(codes.shape[-4:]) != (cfg.n_kv_heads, blocks, 2, cfg.head_dim) or tuple(units.shape[-2:]) != (cfg.n_kv_heads, blocks) \
+                    or codes.shape[:-4].numel() != self.n_layers or units.shape[:-2].numel() != self.n_layers:
+                raise RsError(-1, f"codes {codes.dtype} {list(codes.shape)}, units {units.dtype} {list(units.shape)}: not [{self.n_layers}, "
+                                  f"{cfg.n_kv_heads}, blocks, 2, {cfg.head_dim}] int8 and [{self.n_layers}, {cfg.n_kv_heads}, blocks] fp32, contiguous")
+        _check(load_library().rs_kv_attach_bounds(self.handle, _ptr(codes), _ptr(units), blocks if codes is not None else 0))
+        self.bounds_memory = (codes, units)   # (kept alive)
+
+    def new_bounds(self, capacity_tokens: int):
+        """Memory for the bounds of capacity_tokens tokens in every layer, attached; returns (codes, units)."""
+        import torch
+        cfg, blocks = self.ctx.cfg, max(1, capacity_tokens // 64)
+        codes = torch.empty((self.n_layers, cfg.n_kv_heads, blocks, 2, cfg.head_dim), dtype=torch.int8, device="cuda")
+        units = torch.empty((self.n_layers, cfg.n_kv_heads, blocks), dtype=torch.float32, device="cuda")
+        self.attach_bounds(codes, units)
+        return codes, units
+
+    def bounded(self, layer: int = 0) -> int:
+        """Blocks of `layer` whose bounds are there."""
+        return load_library().rs_kv_bounded(self.handle, layer)
+
+    @property
+    def n_layers(self) -> int:
+        n = 0
+        while load_library().rs_kv_len(self.handle, n) >= 0:
+            n += 1
+        return n
 
     @property
     def is_fp8(self) -> bool:
@@ -477,6 +632,73 @@ class Context:
         _check(self.lib.rs_lm_head(self.handle, _ptr(final_norm_gain), _ptr(w_lm), vocab, _ptr(x_rows), n, _ptr(logits),
                                    _ptr(ws), ws.numel(), _stream_handle(stream)))
         return logits
+
+    # ---- operators on caches (include/rserve_attend.h)
+    def rotary(self, cfg: RotaryConfig) -> Rotary:
+        return Rotary(self, cfg)
+
+    def kv_append(self, layer: int, kvs, lens, q, k, v, q_out, rotary: Optional[Rotary] = None, starts=None, positions=None, stream=None):
+        """Rotates new tokens' queries and keys, and stores keys and values into the caches.  kvs: caches or a CacheSet; lens: new tokens per
+        request; q, q_out: bf16 rows of all query heads (both None: none), k, v: of all KV heads, rows possibly strided; starts: first
+        cache slots (None: at the end; else later tokens are dropped); positions: rotary positions per row (None: the slots)."""
+        cs, cfg = _cache_set(kvs), self.cfg
+        rows, qw, kw = int(k.shape[0]), cfg.n_q_heads * cfg.head_dim, cfg.n_kv_heads * cfg.head_dim
+        n = _ints(lens, len(cs), "lens")
+        if sum(n[: len(cs)]) != rows:
+            raise RsError(-1, f"lens add up to {sum(n[: len(cs)])}, k has {rows} rows")
+        st, ps = _ints(starts, len(cs), "starts"), None
+        if positions is not None:
+            ps = _ints(positions.tolist() if hasattr(positions, "tolist") else positions, rows, "positions")
+        qp, ldq = _rows(q, "q", rows, qw) if q is not None else (None, 0)
+        op, ldo = _rows(q_out, "q_out", rows, qw) if q_out is not None else (None, 0)
+        kp, ldk = _rows(k, "k", rows, kw)
+        vp, ldv = _rows(v, "v", rows, kw)
+        _check(self.lib.rs_kv_append(self.handle, rotary.handle if rotary is not None else None, layer, cs.handles, st, n, len(cs), ps, qp, ldq, kp, ldk, vp,
+                                     ldv, op, ldo, _stream_handle(stream)))
+        return q_out
+
+    def attend_workspace(self, max_rows: int, max_requests: int = 1, fp8_visible_tokens: int = 0, n_blocks: int = 0):
+        """Device workspace for attend (n_blocks = 0) or attend_blocks calls of up to that many rows, requests and blocks; with 8-bit caches and
+        requests of more than a few rows also room for the bf16 expansion of fp8_visible_tokens cached tokens."""
+        import torch
+        return torch.empty(self.lib.rs_attend_workspace_bytes(self.handle, max_rows, max_requests, fp8_visible_tokens, n_blocks), dtype=torch.uint8,
+                           device="cuda")
+
+    def attend(self, layer: int, kvs, lens, q, out, workspace, scale: float = 0.0, stream=None):
+        """Attention of every request's last lens[i] cached tokens over its cache; q, out: bf16 rows of all query heads; scale 0: 1/sqrt(d)."""
+        cs, width = _cache_set(kvs), self.cfg.n_q_heads * self.cfg.head_dim
+        rows = int(q.shape[0])
+        n = _ints(lens, len(cs), "lens")
+        if sum(n[: len(cs)]) != rows:
+            raise RsError(-1, f"lens add up to {sum(n[: len(cs)])}, q has {rows} rows")
+        qp, ldq = _rows(q, "q", rows, width)
+        op, ldo = _rows(out, "out", rows, width)
+        _check(self.lib.rs_attend(self.handle, layer, cs.handles, n, len(cs), qp, ldq, op, ldo, scale, _ptr(workspace), workspace.numel(),
+                                  _stream_handle(stream)))
+        return out
+
+    def bounds_update(self, layer: int, kvs, firsts=None, stream=None):
+        """Bounds on the keys of the caches' finished blocks: of those that have none, or of those from slots `firsts` on."""
+        cs = _cache_set(kvs)
+        _check(self.lib.rs_kv_bounds_update(self.handle, layer, cs.handles, _ints(firsts, len(cs), "firsts"), len(cs), _stream_handle(stream)))
+
+    def attend_blocks(self, layer: int, kvs, lens, q, out, workspace, n_blocks: int, n_first: int = 1, n_last: int = 2, chosen=None,
+                      scale: float = 0.0, stream=None):
+        """attend over at most n_blocks 64-token blocks per token and KV head: the first n_first, the last n_last, and those with the best
+        scores.  chosen: int32 [rows, Hkv, n_blocks] or None, receives them."""
+        import torch
+        cs, cfg = _cache_set(kvs), self.cfg
+        rows, width = int(q.shape[0]), cfg.n_q_heads * cfg.head_dim
+        n = _ints(lens, len(cs), "lens")
+        if sum(n[: len(cs)]) != rows:
+            raise RsError(-1, f"lens add up to {sum(n[: len(cs)])}, q has {rows} rows")
+        if chosen is not None and (chosen.dtype is not torch.int32 or not chosen.is_contiguous() or chosen.numel() != rows * cfg.n_kv_heads * n_blocks):
+            raise RsError(-1, f"chosen must be contiguous int32 [{rows}, {cfg.n_kv_heads}, {n_blocks}]: {chosen.dtype} {list(chosen.shape)}")
+        qp, ldq = _rows(q, "q", rows, width)
+        op, ldo = _rows(out, "out", rows, width)
+        _check(self.lib.rs_attend_blocks(self.handle, layer, cs.handles, n, len(cs), qp, ldq, op, ldo, n_blocks, n_first, n_last, scale, _ptr(chosen),
+                                         _ptr(workspace), workspace.numel(), _stream_handle(stream)))
+        return out
 
 
 class Scheduler:

@@ -4,9 +4,11 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
 
 PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 SRCS = [os.path.join(PKG_DIR, "csrc", "rserve_prefill.hip"),   # kernels + the prefill ABI
+        os.path.join(PKG_DIR, "csrc", "rserve_attend.hip"),    # the operators on caches: kernels + ABI
         os.path.join(PKG_DIR, "csrc", "rserve_sched.cpp")]     # host-only scheduler / tracker ABI
 LIB = os.path.join(PKG_DIR, "librserve_prefill.so")
 
@@ -50,16 +52,27 @@ def build(verbose: bool = True, sanitize_host_to: str = "") -> str:
         if proc.returncode != 0:
             raise RuntimeError("hipcc failed:\n" + proc.stderr)
         return sanitize_host_to
-    cmd = [hipcc] + HIPCC_FLAGS + SRCS + ["-o", LIB + ".tmp"]
-    if verbose:
-        print("[build]", " ".join(cmd), flush=True)
-    proc = subprocess.run(cmd, capture_output=True, text=True)
     noise = "is not a recognized feature for this target"
-    err = "\n".join(l for l in proc.stderr.splitlines() if noise not in l)
-    if proc.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + err)
-    if verbose and err.strip():
-        print(err, file=sys.stderr)
+
+    def finish(what, proc):
+        err = "\n".join(l for l in proc.communicate()[1].splitlines() if noise not in l)
+        if proc.returncode != 0:
+            raise RuntimeError(what + " failed:\n" + err)
+        if verbose and err.strip():
+            print(err, file=sys.stderr)
+
+    def start(cmd):
+        if verbose:
+            print("[build]", " ".join(cmd), flush=True)
+        return subprocess.Popen(cmd, stdout=subprocess.DEVNULL, stderr=subprocess.PIPE, text=True)
+
+    with tempfile.TemporaryDirectory() as tmp:   # the sources side by side, then one link
+        objs = [os.path.join(tmp, os.path.basename(src) + ".o") for src in SRCS]
+        compile_flags = [f for f in HIPCC_FLAGS if f != "-shared"]
+        procs = [start([hipcc] + compile_flags + ["-c", src, "-o", obj]) for src, obj in zip(SRCS, objs)]
+        for src, proc in zip(SRCS, procs):
+            finish("hipcc on " + os.path.basename(src), proc)
+        finish("linking", start([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC"] + objs + ["-o", LIB + ".tmp"]))
     os.replace(LIB + ".tmp", LIB)
     return LIB
 

@@ -25,6 +25,7 @@
 
 #include "attention_plan.h"
 #include "common.h"
+#include "exact_row.h"
 
 struct ReqDesc {
     int row0;       // first row of this request in the packed [sum T, ...] activations
@@ -135,14 +136,17 @@ struct AttnPartial {
 // running maximum of the whole-tile kernel: 313), 1200 on 0: 45.7 -> 39.7, 2048 on 2000: 217 -> 206; 7B, 2048 on 0: 47.7 -> 46.0.
 constexpr float ATT_RESCALE_SUM = 256.0f, ATT_HEADROOM_LOG2 = 6.0f;
 
-template <int D, bool MAY_PAGE, int WAVES>
+// ROWS: the output is row-major and final, for a caller instead of the output projection: rows that are not finite are taken again
+// one by one, so that what a query does not see does not reach it (a masked key's weight is zero, but zero times an infinite or
+// NaN value is NaN; the layer has no use for rows behind such a token).
+template <int D, bool MAY_PAGE, int WAVES, bool ROWS = false>
 __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_pipelined_kernel(const ReqDesc* __restrict__ reqs,
                                                                                 const AttnItem* __restrict__ items,
                                                                                 const bf16* __restrict__ qkv, int ld_qkv,
                                                                                 bf16* __restrict__ out, int ld_out,
                                                                                 int g, float scale_log2e,
                                                                                 float* __restrict__ split_buf) {
-    constexpr int ROWS = 32 * WAVES, THREADS = 64 * WAVES;
+    constexpr int BLOCK_ROWS = 32 * WAVES, THREADS = 64 * WAVES;
     constexpr int KSTEPS = D / 16;
     constexpr int DT = D / 32;
     constexpr int K_ROW_BYTES = D * 2;
@@ -166,7 +170,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_pipelined_kernel(c
     const AttnItem item = items[blockIdx.x];
     const ReqDesc rq = reqs[item.req];
     const int rows_total = rq.T * g;
-    const int wrow0 = item.qblock * ROWS + wave * 32;
+    const int wrow0 = item.qblock * BLOCK_ROWS + wave * 32;
     const int row = wrow0 + l32;
     const int row_c = min(row, rows_total - 1);
     const int tok = row_c / g;
@@ -432,6 +436,45 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_pipelined_kernel(c
     }
 
     const float l_tot = l_run + __shfl_xor(l_run, 32, WAVE);
+    if constexpr (ROWS) {
+        bool bad = !(fabsf(l_tot) <= 3.402823466e38f);
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) bad |= !(fabsf(acc_o[t][r]) <= 3.402823466e38f);
+        const unsigned long long any = __builtin_amdgcn_ballot_w64(bad && row < rows_total);
+        const uint32_t again = (uint32_t)any | (uint32_t)(any >> 32);   // rows of the wavefront
+        if (__builtin_expect(again != 0, 0)) {
+            for (int i = 0; i < 32; ++i) {
+                if (!((again >> i) & 1u)) continue;
+                const int arow = wrow0 + i, atok = arow / g, ahead = item.kvh * g + (arow - atok * g);
+                const auto tile_at = [&](int kb, global_bytes& kt, global_bytes& vt, int& block) RS_INLINE {
+                    const int index = tiles.template index_of<MAY_PAGE>(kb);
+                    kt = (global_bytes)tiles.template k_tile<MAY_PAGE>(index);
+                    vt = (global_bytes)tiles.template v_tile<MAY_PAGE>(index);
+                    block = kb;
+                    return true;
+                };
+                float em, el, eo[D / 64];
+                exact_row<D, false>(qkv + (size_t)(rq.row0 + atok) * ld_qkv + ahead * D, scale_log2e, rq.P + atok, kb0, nkb, tile_at, em, el, eo);
+                if (item.slot >= 0) {
+                    float* const slot = split_buf + (size_t)item.slot * AttnPartial<D>::SLOT_FLOATS;
+                    const int rs = wave * 32 + i;
+#pragma unroll
+                    for (int j = 0; j < D / 64; ++j) slot[((size_t)((lane >> 2) + 16 * j) * BLOCK_ROWS + rs) * 4 + (lane & 3)] = eo[j];
+                    if (lane == 0) {
+                        slot[(size_t)D * BLOCK_ROWS + rs] = fmaxf(em / scale_log2e, -3.402823466e38f);
+                        slot[(size_t)(D + 1) * BLOCK_ROWS + rs] = el;
+                    }
+                } else {
+                    bf16* const op = out + (size_t)(rq.row0 + atok) * ld_out + ahead * D;
+#pragma unroll
+                    for (int j = 0; j < D / 64; ++j) op[lane + 64 * j] = f32_to_bf16(eo[j] / el);
+                }
+            }
+            if ((again >> l32) & 1u) return;   // (this lane's row is done)
+        }
+    }
     if (item.slot >= 0) {
         // a part of a split block: unnormalised output, reference maximum and row sum go to the slot (all 32 rows of
         // the wavefront, clamped duplicates included: the merge kernel decides what is stored; wavefronts without rows left above)
@@ -443,16 +486,29 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_pipelined_kernel(c
             for (int q = 0; q < 4; ++q) {
                 const f32x4 o = {acc_o[t][4 * q], acc_o[t][4 * q + 1], acc_o[t][4 * q + 2], acc_o[t][4 * q + 3]};
                 // chunk (features 32t + 8q + 4half .. +3) of row rs
-                *reinterpret_cast<f32x4*>(slot + ((size_t)(t * 8 + q * 2 + half) * ROWS + rs) * 4) = o;
+                *reinterpret_cast<f32x4*>(slot + ((size_t)(t * 8 + q * 2 + half) * BLOCK_ROWS + rs) * 4) = o;
             }
         if (half == 0) {
-            slot[(size_t)D * ROWS + rs] = m_ref;
-            slot[(size_t)(D + 1) * ROWS + rs] = l_tot;
+            slot[(size_t)D * BLOCK_ROWS + rs] = m_ref;
+            slot[(size_t)(D + 1) * BLOCK_ROWS + rs] = l_tot;
         }
         return;
     }
     if (row < rows_total) {
         const float inv = 1.0f / l_tot;
+        if constexpr (ROWS) {
+            bf16* const op = out + (size_t)(rq.row0 + tok) * ld_out + head * D + half * 4;
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    bf16x4 o;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[e] = f32_to_bf16(acc_o[t][4 * q + e] * inv);
+                    *reinterpret_cast<bf16x4*>(op + t * 32 + q * 8) = o;
+                }
+            return;
+        }
         const uint32_t m = (uint32_t)(rq.row0 + tok);
         char* op = reinterpret_cast<char*>(out) + (size_t)(m >> 5) * (size_t)(ld_out >> 4) * 1024 + (m & 31u) * 16u + half * 8;
         const int ks0 = (head * D) >> 4;
@@ -479,7 +535,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_pipelined_kernel(c
 constexpr int ATT_MERGE_Y = 16;
 constexpr int ATT_FEW_PARTS = 4;
 constexpr int ATT_MERGE_EARLY_WAVES = 12;   // wavefronts per compute unit that the early form's registers leave room for
-template <int D, int WAVES, int MAXP, bool EARLY>
+template <int D, int WAVES, int MAXP, bool EARLY, bool ROW_MAJOR = false>
 __global__ __launch_bounds__(32 * WAVES) void attn_merge_kernel(const ReqDesc* __restrict__ reqs, const AttnMergeItem* __restrict__ items,
                                                          const float* __restrict__ split_buf, bf16* __restrict__ out, int ld_out,
                                                          int g, float scale_log2e) {
@@ -543,6 +599,10 @@ __global__ __launch_bounds__(32 * WAVES) void attn_merge_kernel(const ReqDesc* _
 #pragma unroll
         for (int e = 0; e < 4; ++e) o4[e] = f32_to_bf16(acc[e] * inv);
         // chunk c = 8t + 2q + half holds features 32t + 8q + 4half .. +3: the same place the unsplit kernel writes
+        if constexpr (ROW_MAJOR) {
+            *reinterpret_cast<bf16x4*>(out + (size_t)m * ld_out + head * D + 4 * c) = o4;
+            continue;
+        }
         const int t = c >> 3, q = (c >> 1) & 3, hf = c & 1;
         *reinterpret_cast<bf16x4*>(op + hf * 8 + (size_t)(((ks0 + 2 * t + (q >> 1)) * 2 + (q & 1)) * 512)) = o4;
     }

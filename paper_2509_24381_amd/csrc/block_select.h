@@ -1,0 +1,248 @@
+// Which blocks a token attends to: bounds on the keys of finished blocks, and the selection from them.
+#pragma once
+#include "attend_few.h"
+#include "common.h"
+
+typedef __attribute__((ext_vector_type(4))) int i32x4;
+
+constexpr float BOUND_LIMIT = 1.2676506002282294e30f;   // 2^100
+constexpr int BOUND_LEAST = -100;
+
+// The smallest e >= -100 with top <= 127 * 2^e  (0 <= top <= 2^100).
+RS_DEVICE int code_exponent(float top) {
+    // top = m 2^x, m in [1/2, 1): e = x - 7 where 128 m <= 127, x - 6 above
+    const int x = __builtin_amdgcn_frexp_expf(top);
+    const int e = x - 7 + (__builtin_amdgcn_frexp_mantf(top) * 128.0f > 127.0f ? 1 : 0);
+    return top <= 127.0f / BOUND_LIMIT ? BOUND_LEAST : e;
+}
+RS_DEVICE float limited(float x) { return x == x ? fminf(fmaxf(x, -BOUND_LIMIT), BOUND_LIMIT) : 0.0f; }
+
+// ---------------------------------------------------------------- bounds
+// One wavefront per (block, KV head), bound by reading K once: all of a tile's loads are in flight together, a lane holding 8 (8-bit: 16)
+// features of a sixteenth (an eighth) of the keys.  Maxima and minima do not depend on the order they are taken in, and
+// codes are whole numbers: the result is the same bits whatever computes it.
+struct BoundsReq {          // 64 bytes: a FewReq with the bounds' memory in it
+    uint64_t k;
+    uint64_t head_bytes;
+    uint32_t block_bytes;
+    int32_t pages;
+    uint64_t codes, units;  // of the layer
+    int32_t room;           // blocks from a KV head's bounds to the next head's
+    int32_t first;          // first block
+    float k_scale;
+    int32_t pad_[3];
+};
+static_assert(sizeof(BoundsReq) == 64, "sixteen words");
+
+template <int D, bool FP8>
+__global__ __launch_bounds__(256) void key_bounds_kernel(int n_req, int hkv, int items, InlineTable tab) {
+    constexpr int F = FP8 ? 16 : 8, CH = D / F, STEP = 64 / CH, N = 64 / STEP;   // features of a lane, lanes per key, keys per load, loads
+    const uint32_t* const table = tab.w;
+    const int lane = threadIdx.x & 63, id = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (id >= items) return;
+    const int r = request_of(table, n_req, (uint32_t)id);
+    const BoundsReq rq = reinterpret_cast<const BoundsReq*>(table + table_reqs_at(n_req))[r];
+    const int local = id - (int)table[r], h = local % hkv, block = rq.first + local / hkv;
+    const uint64_t index = rq.pages == CONTIGUOUS ? (uint32_t)block : table[rq.pages + block];
+    global_bytes kt = (global_bytes)(rq.k + (uint64_t)h * rq.head_bytes + index * rq.block_bytes);
+    uint4 v[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = ld_tile_16(kt + (size_t)i * 1024 + lane * 16);
+    const auto value = [&](const uint4& w, int e) RS_INLINE {
+        const uint32_t x = e * (FP8 ? 1 : 2) / 4 == 0 ? w.x : e * (FP8 ? 1 : 2) / 4 == 1 ? w.y : e * (FP8 ? 1 : 2) / 4 == 2 ? w.z : w.w;
+        if constexpr (FP8) {
+            const f32x2 p = (e & 2) ? __builtin_amdgcn_cvt_pk_f32_fp8((int)x, true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)x, false);
+            return p[e & 1] * rq.k_scale;
+        } else {
+            return __builtin_bit_cast(float, (e & 1) ? x & 0xffff0000u : x << 16);
+        }
+    };
+    float hi[F], lo[F];
+#pragma unroll
+    for (int e = 0; e < F; ++e) {
+        hi[e] = -INFINITY;
+        lo[e] = INFINITY;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float x = limited(value(v[i], e));
+            hi[e] = fmaxf(hi[e], x);
+            lo[e] = fminf(lo[e], x);
+        }
+#pragma unroll
+        for (int off = CH; off < 64; off <<= 1) {
+            hi[e] = fmaxf(hi[e], __shfl_xor(hi[e], off, WAVE));
+            lo[e] = fminf(lo[e], __shfl_xor(lo[e], off, WAVE));
+        }
+    }
+    float top = 0.0f;
+#pragma unroll
+    for (int e = 0; e < F; ++e) top = fmaxf(top, fmaxf(hi[e], -lo[e]));
+#pragma unroll
+    for (int off = 1; off < CH; off <<= 1) top = fmaxf(top, __shfl_xor(top, off, WAVE));
+    const int ex = code_exponent(top);
+    int8_t* const codes = reinterpret_cast<int8_t*>(rq.codes) + ((size_t)h * rq.room + block) * 2 * D;
+    if (lane < CH) {
+        union { int8_t b[F]; uint32_t w[F / 4]; } ch, cl;
+#pragma unroll
+        for (int e = 0; e < F; ++e) {
+            ch.b[e] = (int8_t)(int)ceilf(__builtin_ldexpf(hi[e], -ex));
+            cl.b[e] = (int8_t)(int)floorf(__builtin_ldexpf(lo[e], -ex));
+        }
+#pragma unroll
+        for (int i = 0; i < F / 4; ++i) {
+            reinterpret_cast<uint32_t*>(codes + lane * F)[i] = ch.w[i];
+            reinterpret_cast<uint32_t*>(codes + D + lane * F)[i] = cl.w[i];
+        }
+    }
+    if (lane == 0) reinterpret_cast<float*>(rq.units)[(size_t)h * rq.room + block] = __builtin_ldexpf(1.0f, ex);
+}
+
+// ---------------------------------------------------------------- selection
+// One workgroup per (KV head, a few consecutive tokens of a request).
+//  1. every token's p and n (see the score in the header), int8, into LDS;
+//  2. scores of 16 blocks x 16 tokens per v_mfma_i32_16x16x64_i8 chain (the contraction runs over high and low codes), as keys
+//     that order like the scores, into LDS;
+//  3. a wavefront per token finds the score that the last selected block has, by bisection over the key's bits, and writes the blocks
+//     down in ascending order.
+struct SelectReq {          // 64 bytes
+    uint64_t codes, units;
+    int32_t room;
+    int32_t row0, T, P;
+    int32_t pad_[8];
+};
+static_assert(sizeof(SelectReq) == 64, "sixteen words");
+struct SelectArgs {
+    int n_req, hkv, g, halvings;
+    const bf16* q;
+    long ld_q;
+    int tokens;             // tokens of a workgroup, at most 16
+    int blocks;             // keys there is room for per token in LDS
+    int n_blocks, n_first, n_last;
+    int* chosen;
+    // the attention kernel's table, from the staging buffer to the workspace: workgroups (x >= groups, y = 0) copy it
+    const uint4* copy_from;
+    uint4* copy_to;
+    int copy_chunks, groups;
+};
+
+RS_DEVICE uint32_t key_of_score(float s) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, s + 0.0f);   // (minus zero is zero)
+    return (b & 0x80000000u) ? ~b : b | 0x80000000u;
+}
+
+template <int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void block_select_kernel(SelectArgs a, InlineTable tab) {
+    extern __shared__ __attribute__((aligned(16))) uint32_t keys[];   // [tokens][blocks]
+    __shared__ __attribute__((aligned(16))) int8_t u[16][2 * D];
+    const uint32_t* const table = tab.w;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = blockIdx.y;
+    if ((int)blockIdx.x >= a.groups) {
+        const int i = ((int)blockIdx.x - a.groups) * 64 * WAVES + (int)threadIdx.x;
+        if (h == 0 && i < a.copy_chunks) a.copy_to[i] = a.copy_from[i];
+        return;
+    }
+    const int req = request_of(table, a.n_req, blockIdx.x);
+    const SelectReq rq = reinterpret_cast<const SelectReq*>(table + table_reqs_at(a.n_req))[req];
+    const int t0 = (int)(blockIdx.x - table[req]) * a.tokens, nt = min(a.tokens, rq.T - t0);
+    const int b_last = (rq.P + t0 + nt - 1) / 64;          // own block of the last token
+    // blocks that can need a score
+    const int s0 = min(a.n_first, b_last), s1 = max(s0, b_last + 1 - a.n_last);
+    const bool scored = b_last + 1 > a.n_blocks && s1 > s0;   // (else every token takes all it has, or none but the forced ones)
+    if (scored) {
+        constexpr int W = D / 64;   // features of a lane: lane W ..
+        for (int t = wave; t < 16; t += WAVES) {
+            int p[W] = {}, n[W] = {};
+            if (t < nt) {
+                const bf16* const src = a.q + (size_t)(rq.row0 + t0 + t) * a.ld_q + (size_t)h * a.g * D + lane * W;
+                float top = 0.0f;
+                for (int i = 0; i < a.g; ++i)
+#pragma unroll
+                    for (int j = 0; j < W; ++j) top = fmaxf(top, fabsf(limited(bf16_to_f32(src[i * D + j]))));
+#pragma unroll
+                for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, WAVE));
+                const int ex = code_exponent(top);
+                for (int i = 0; i < a.g; ++i)
+#pragma unroll
+                    for (int j = 0; j < W; ++j) {
+                        const int code = (int)rintf(__builtin_ldexpf(limited(bf16_to_f32(src[i * D + j])), -ex));
+                        p[j] += max(code, 0);
+                        n[j] += max(-code, 0);
+                    }
+            }
+            const int half = (1 << a.halvings) >> 1;
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+                u[t][lane * W + j] = (int8_t)((p[j] + half) >> a.halvings);
+                u[t][D + lane * W + j] = (int8_t)(-((n[j] + half) >> a.halvings));
+            }
+        }
+        __syncthreads();
+        const int r = lane & 15, c = lane >> 4;
+        i32x4 uf[2 * D / 64];
+#pragma unroll
+        for (int k = 0; k < 2 * D / 64; ++k) uf[k] = *reinterpret_cast<const i32x4*>(&u[r][k * 64 + c * 16]);
+        const int8_t* const codes = reinterpret_cast<const int8_t*>(rq.codes) + (size_t)h * rq.room * 2 * D;
+        const float* const units = reinterpret_cast<const float*>(rq.units) + (size_t)h * rq.room;
+        for (int b = s0 + wave * 16; b < s1; b += WAVES * 16) {
+            const int8_t* const src = codes + (size_t)min(b + r, s1 - 1) * 2 * D + c * 16;
+            i32x4 x[2 * D / 64], dot = {0, 0, 0, 0};
+#pragma unroll
+            for (int k = 0; k < 2 * D / 64; ++k) x[k] = *reinterpret_cast<const i32x4*>(src + k * 64);
+            float unit[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) unit[e] = units[min(b + c * 4 + e, s1 - 1)];
+#pragma unroll
+            for (int k = 0; k < 2 * D / 64; ++k) dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[k], uf[k], dot, 0, 0, 0);
+            if (r < nt) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)   // block b + 4 c + e, token r
+                    if (b + c * 4 + e < s1) keys[r * a.blocks + b + c * 4 + e - s0] = key_of_score((float)dot[e] * unit[e]);
+            }
+        }
+        __syncthreads();
+    }
+    for (int t = wave; t < nt; t += WAVES) {
+        const int own = (rq.P + t0 + t) / 64;
+        const int lo = min(a.n_first, own + 1), hi = max(lo, own + 1 - a.n_last);   // blocks lo .. hi - 1 compete
+        const int take = min(max(a.n_blocks - (own + 1 - (hi - lo)), 0), hi - lo);
+        const uint32_t* const key = keys + t * a.blocks - s0;
+        // the take-th largest key: `cut`; of the blocks that have it, the first `equals`
+        uint32_t cut = 0;
+        int equals = 0;
+        if (take > 0 && take < hi - lo) {
+            int above = 0;   // keys above the range that is left
+            uint32_t bit = 0x80000000u;
+            for (; bit; bit >>= 1) {
+                const uint32_t mid = cut | bit;
+                int count = 0;
+                for (int b = lo + lane; b < hi; b += 64) count += key[b] >= mid;
+#pragma unroll
+                for (int off = 32; off > 0; off >>= 1) count += __shfl_xor(count, off, WAVE);
+                if (count >= take) cut = mid;
+                else above = count;
+            }
+            equals = take - above;
+        }
+        int* const out = a.chosen + ((size_t)(rq.row0 + t0 + t) * a.hkv + h) * a.n_blocks;
+        int done = 0;
+        for (int b0 = 0; b0 <= own && done < a.n_blocks; b0 += 64) {
+            const int b = b0 + lane;
+            bool sel = b < lo || (b >= hi && b <= own);
+            if (b >= lo && b < hi) sel = take == hi - lo;
+            bool eq = false;
+            if (take > 0 && take < hi - lo && b >= lo && b < hi) {
+                sel = key[b] > cut;
+                eq = key[b] == cut;
+            }
+            const unsigned long long below = lane == 0 ? 0ull : ~0ull >> (64 - lane);
+            const unsigned long long eqs = __builtin_amdgcn_ballot_w64(eq);
+            if (eq) sel = __popcll(eqs & below) < equals;
+            equals -= min(equals, (int)__popcll(eqs));
+            const unsigned long long sels = __builtin_amdgcn_ballot_w64(sel);
+            const int at = done + (int)__popcll(sels & below);
+            if (sel && at < a.n_blocks) out[at] = b;
+            done += (int)__popcll(sels);
+        }
+        for (int i = min(done, a.n_blocks) + lane; i < a.n_blocks; i += 64) out[i] = -1;
+    }
+}

@@ -160,7 +160,7 @@ __global__ __launch_bounds__(256) void rms_and_fragment_major_kernel(const bf16*
 
 // ---------------------------------------------------------------- first-token head: final RMSNorm + vocabulary projection
 // h[r][k] = x[r][k] * g[k] * rsqrt(mean(x[r]^2) + eps), kept in fp32.  One wavefront per row.
-__global__ __launch_bounds__(256) void final_norm_kernel(const bf16* __restrict__ x, const bf16* __restrict__ gain,
+static __global__ __launch_bounds__(256) void final_norm_kernel(const bf16* __restrict__ x, const bf16* __restrict__ gain,
                                                          float* __restrict__ h, int rows, int H, float eps) {
     const int lane = threadIdx.x & 63;
     const int row = blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -264,7 +264,7 @@ constexpr int LM_MFMA_ROWS = 3;   // from this many rows on
 constexpr int LM_GROUP = 10;      // rows per B operand
 constexpr int LM_MAX_GROUPS = 2;  // B operands per launch (three spill: 525 us for 30 rows, two passes take 470)
 constexpr int LM_VROWS = 64;      // vocabulary rows per workgroup
-__global__ __launch_bounds__(256) void final_norm_split_kernel(const bf16* __restrict__ x, const bf16* __restrict__ gain,
+static __global__ __launch_bounds__(256) void final_norm_split_kernel(const bf16* __restrict__ x, const bf16* __restrict__ gain,
                                                                bf16* __restrict__ hb, int rows, int H, float eps) {
     // one workgroup per place of a group of rows (grid x: LM_GROUP, + 1 for the two columns that hold no row; grid y: groups)
     const int rg = blockIdx.x;
@@ -542,7 +542,7 @@ __global__ __launch_bounds__(256) void append_kv_kernel(const bf16* __restrict__
 // `wide`: the source can be read 16 bytes at a time.
 constexpr int PACK_K = 256;
 enum PackMode { PACK_IDENTITY = 0, PACK_GATE_UP = 1, PACK_QKV_ROPE = 2 };
-__global__ __launch_bounds__(256) void pack_rows_kernel(const bf16* __restrict__ src, const bf16* __restrict__ gain,
+static __global__ __launch_bounds__(256) void pack_rows_kernel(const bf16* __restrict__ src, const bf16* __restrict__ gain,
                                                         bf16* __restrict__ dst, int K, int mode, int p0, int p1, int wide) {
     constexpr int CH = PACK_K / 8;   // 16-byte chunks of a row
     __shared__ uint4 tile[32][CH + 1];   // (rows one chunk further: 16 rows' reads of one chunk cover all banks)

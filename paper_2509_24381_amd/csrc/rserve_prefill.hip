@@ -22,6 +22,7 @@
 #include "gemm_strip.h"
 #include "gemm_skinny.h"
 #include "gemm_tile.h"
+#include "host_state.h"
 #include "last_error.h"
 
 namespace {
@@ -41,18 +42,6 @@ rs_status fail(rs_status st, const char* fmt, ...) {
     va_end(ap);
     return st;
 }
-
-#define RS_HIP(expr)                                                                              \
-    do {                                                                                          \
-        hipError_t e_ = (expr);                                                                   \
-        if (e_ != hipSuccess) return fail(RS_EHIP, "%s: %s", #expr, hipGetErrorString(e_));       \
-    } while (0)
-
-inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
-inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-
-constexpr int RING_SLOTS = 32;
-constexpr int RING_CHECKPOINT = 8;
 
 // Workspace of rs_prefill_chunk_static.  In host code the array's name is only a handle for hipGetSymbolAddress: each GPU
 // holds its own copy at its own address, which static_workspace_lookup fetches once per device (with that device
@@ -86,102 +75,53 @@ rs_status rs_internal_fail(rs_status st, const char* fmt, ...) {
     return st;
 }
 
-struct rs_ctx {
-    rs_layer_cfg cfg;
-    int qkv_dim, q_dim, kv_dim, group;
-    float2* rope_dev = nullptr;  // [max_pos][d/2] (cos, sin)
-    // pinned staging ring for per-call descriptors
-    char* pinned[RING_SLOTS] = {};
-    char* pinned_dev[RING_SLOTS] = {};  // the same buffers as the device addresses them
-    // A slot may be overwritten once the first kernel of the call that used it has run.  Recording an event behind that
-    // kernel in every call would tell, but an event record holds the stream up for about 6 us; so events are recorded only
-    // at checkpoints: after every RING_CHECKPOINT-th use, and - on the stream that is being left - whenever the caller's
-    // stream changes.  Uses are numbered; the first checkpoint at or after use u is on u's stream and behind its kernel.
-    hipEvent_t slot_done[RING_SLOTS] = {};
-    long slot_recorded_at[RING_SLOTS];   // the use number slot_done[slot] was last recorded at (-1: never)
-    size_t slot_bytes = 0;
-    long use_count = 0;                   // uses so far; use u occupies slot u % RING_SLOTS
-    hipStream_t last_stream = nullptr;
-    int splitk_override = 0;  // RS_SPLITK environment variable (0 = heuristic)
-    int mrope_b0 = 0, mrope_b1 = 0;  // rotary pair j turns with axis 0 below b0, axis 1 below b1, axis 2 above (set in rs_ctx_create)
-    bool attn_plain_order = false;  // RS_ATTN_ORDER=plain: attention blocks that share a compute unit stay heaviest-first (no pairing)
-    int attn_split = 0;       // RS_ATTN_SPLIT environment variable: parts a block's key range is cut into (0: decided per call)
-    int gemm_few = 1;         // RS_NARROW environment variable: 0 keeps every call on the strip GEMMs (no tiles, no few-rows kernel)
-    int n_cu = 256;           // compute units of the device: the number of strips a GEMM launch is cut into
-    bool has_device = false;  // false: created on a host without a GPU; argument checks work, launches return RS_EHIP
-    int device = -1;          // the GPU that was current in rs_ctx_create
-    void* static_ws = nullptr;  // that GPU's copy of the static workspace (rs_prefill_chunk_static)
-    int lm_rows = 0;          // rows per launch of the first-token head (0: its LDS size not yet set, see rs_lm_head)
-    // measurement hook: HIP events around every launch of one step of the layer
-    int prof_step = -1;
-    int prof_count = 0;
-    int prof_every = 1;       // measure every n-th launch of the step
-    int prof_seen = 0;        // launches of the step seen since rs_profile_enable
-    bool prof_take = false;   // the launch in progress is being measured
-    std::vector<hipEvent_t> prof_events;  // (start, stop) pairs
-};
+rs_status ring_acquire(rs_ctx* ctx, hipStream_t st, int* slot_out) {
+    const long use = ctx->use_count;
+    if (use > 0 && st != ctx->last_stream) {  // leaving a stream: a checkpoint behind its last use, unless there is one
+        const int prev = (int)((use - 1) % RING_SLOTS);
+        if (ctx->slot_recorded_at[prev] != use - 1) {
+            if (hipEventRecord(ctx->slot_done[prev], ctx->last_stream) != hipSuccess) {
+                (void)hipGetLastError();       // (the stream is gone: wait for everything instead)
+                RS_HIP(hipDeviceSynchronize());
+                RS_HIP(hipEventRecord(ctx->slot_done[prev], st));
+            }
+            ctx->slot_recorded_at[prev] = use - 1;
+        }
+    }
+    if (use >= RING_SLOTS) {  // the slot's previous use: wait for the first checkpoint at or after it
+        const long old = use - RING_SLOTS;
+        bool waited = false;
+        for (long u = old; u < old + RING_CHECKPOINT && !waited; ++u)
+            if (ctx->slot_recorded_at[u % RING_SLOTS] == u) {
+                RS_HIP(hipEventSynchronize(ctx->slot_done[u % RING_SLOTS]));
+                waited = true;
+            }
+        if (!waited) return fail(RS_EINVAL, "internal: no checkpoint behind use %ld of the descriptor ring", old);
+    }
+    *slot_out = (int)(use % RING_SLOTS);
+    return RS_OK;
+}
 
-// A pool of fixed-size pages in caller-owned device memory.  A page holds 64 tokens of ONE layer: the K tiles [64][d] of
-// all KV heads followed by their V^T tiles [d][64].  The free list lives on the host.
-struct rs_kv_pool {
-    rs_ctx* ctx;
-    char* base;
-    size_t page_bytes;
-    int n_pages;
-    bool fp8 = false;              // pages of E4M3 bytes (half the size) for 8-bit caches
-    int n_caches = 0;              // paged caches alive on this pool
-    std::vector<int> free_pages;   // stack: the back is handed out next
-};
+rs_status ring_commit(rs_ctx* ctx, hipStream_t st) {
+    const long use = ctx->use_count;
+    const int slot = (int)(use % RING_SLOTS);
+    if (use % RING_CHECKPOINT == RING_CHECKPOINT - 1) {
+        RS_HIP(hipEventRecord(ctx->slot_done[slot], st));
+        ctx->slot_recorded_at[slot] = use;
+    } else {
+        ctx->slot_recorded_at[slot] = -1;   // (what was recorded here belonged to the slot's previous use)
+    }
+    ctx->last_stream = st;
+    ctx->use_count = use + 1;
+    return RS_OK;
+}
 
-struct rs_kv {
-    rs_ctx* ctx;
-    int n_layers;
-    int cap;  // contiguous: capacity in tokens, multiple of 64; paged: unused (see capacity())
-    char* base;
-    size_t k_bytes;      // one layer's K
-    size_t layer_bytes;  // K + V^T
-    std::vector<int> len;
-    rs_kv_pool* pool = nullptr;             // paged caches only
-    std::vector<std::vector<int>> pages;    // paged: pages[layer][block]
-    bool fp8 = false;                       // one E4M3 byte per element (contiguous caches only); k_bytes counts bytes
-    float k_scale = 1.0f, v_scale = 1.0f;   // 8-bit caches: value = decode(code) * scale
-    bool paged() const { return pool != nullptr; }
-    uint8_t* kc_of(int layer) const { return reinterpret_cast<uint8_t*>(base + (size_t)layer * layer_bytes); }
-    uint8_t* vc_of(int layer) const { return reinterpret_cast<uint8_t*>(base + (size_t)layer * layer_bytes + k_bytes); }
-    bf16* k_of(int layer) const { return reinterpret_cast<bf16*>(base + (size_t)layer * layer_bytes); }
-    bf16* vt_of(int layer) const { return reinterpret_cast<bf16*>(base + (size_t)layer * layer_bytes + k_bytes); }
-    // new pages layer `layer` needs before it can hold n_tokens
-    int pages_missing(int layer, long n_tokens) const {
-        return paged() ? std::max<long>(0, (n_tokens + 63) / 64 - (long)pages[layer].size()) : 0;
-    }
-    void take_pages(int layer, long n_tokens) {  // the caller has checked that the pool has enough
-        for (int k = pages_missing(layer, n_tokens); k > 0; --k) {
-            pages[layer].push_back(pool->free_pages.back());
-            pool->free_pages.pop_back();
-        }
-    }
-    void give_back_pages(int layer, long n_tokens) {  // keeps the pages that hold the first n_tokens
-        const size_t keep = (size_t)((n_tokens + 63) / 64);
-        while (pages[layer].size() > keep) {
-            pool->free_pages.push_back(pages[layer].back());
-            pages[layer].pop_back();
-        }
-    }
-    // the cache of `layer` as the kernels see it (row0 / T / P left to the caller; `pages` is a device pointer or a marker)
-    ReqDesc view(int layer, const int* dev_pages) const {
-        ReqDesc d{};
-        d.cap = cap;
-        d.hkv = ctx->cfg.n_kv_heads;
-        if (paged()) {
-            d.kcache = reinterpret_cast<bf16*>(pool->base);
-            d.pages = dev_pages;
-        } else {
-            d.kcache = k_of(layer);
-            d.vtcache = vt_of(layer);
-        }
-        return d;
-    }
-};
+rs_status refuse_capture(hipStream_t st) {
+    hipStreamCaptureStatus capturing = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(st, &capturing) != hipSuccess) (void)hipGetLastError();
+    else if (capturing != hipStreamCaptureStatusNone) return fail(RS_ESTATE, "the stream is capturing a HIP graph");
+    return RS_OK;
+}
 
 namespace {
 
@@ -662,6 +602,13 @@ rs_status import_check(const rs_kv* kv, int layer, int n_tokens) {
     return RS_OK;
 }
 
+// The layer's content is new, and V behind it zero.
+void imported(rs_kv* kv, int layer, int n_tokens) {
+    kv->dropped_from(layer, 0);
+    kv->len[layer] = n_tokens;
+    kv->stale_tail[layer] = 0;
+}
+
 // Runs the export or import kernel over tokens [0, n): in one launch for a contiguous cache, in windows of
 // KV_PAGE_WINDOW blocks (whose page numbers ride in the kernel arguments) for a paged one.
 template <class Launch>
@@ -781,9 +728,8 @@ rs_status prefill_enqueue(rs_ctx* ctx, const rs_layer_weights* w, int layer, rs_
     const rs_layer_cfg& f = ctx->cfg;
     const WorkspaceLayout L = ws_layout(ctx, T, R);
     {   // a call recorded into a HIP graph would replay with stale descriptors: refuse it, before anything changes
-        hipStreamCaptureStatus capturing = hipStreamCaptureStatusNone;
-        if (hipStreamIsCapturing(reinterpret_cast<hipStream_t>(stream), &capturing) != hipSuccess) (void)hipGetLastError();
-        else if (capturing != hipStreamCaptureStatusNone) return fail(RS_ESTATE, "the stream is capturing a HIP graph");
+        const rs_status s = refuse_capture(reinterpret_cast<hipStream_t>(stream));
+        if (s != RS_OK) return s;
     }
 
     // Pages taken below go back to their pools if a later host-side check refuses the call (nothing may change on a
@@ -891,29 +837,9 @@ rs_status prefill_enqueue(rs_ctx* ctx, const rs_layer_weights* w, int layer, rs_
         return fail(RS_EINVAL, "internal: descriptor sizing");
 
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    const long use = ctx->use_count;
-    const int slot = (int)(use % RING_SLOTS);
-    if (use > 0 && st != ctx->last_stream) {  // leaving a stream: a checkpoint behind its last use, unless there is one
-        const int prev = (int)((use - 1) % RING_SLOTS);
-        if (ctx->slot_recorded_at[prev] != use - 1) {
-            if (hipEventRecord(ctx->slot_done[prev], ctx->last_stream) != hipSuccess) {
-                (void)hipGetLastError();       // (the stream is gone: wait for everything instead)
-                RS_HIP(hipDeviceSynchronize());
-                RS_HIP(hipEventRecord(ctx->slot_done[prev], st));
-            }
-            ctx->slot_recorded_at[prev] = use - 1;
-        }
-    }
-    if (use >= RING_SLOTS) {  // the slot's previous use: wait for the first checkpoint at or after it
-        const long old = use - RING_SLOTS;
-        bool waited = false;
-        for (long u = old; u < old + RING_CHECKPOINT && !waited; ++u)
-            if (ctx->slot_recorded_at[u % RING_SLOTS] == u) {
-                RS_HIP(hipEventSynchronize(ctx->slot_done[u % RING_SLOTS]));
-                waited = true;
-            }
-        if (!waited) return fail(RS_EINVAL, "internal: no checkpoint behind use %ld of the descriptor ring", old);
-    }
+    int slot = 0;
+    rs_status s = ring_acquire(ctx, st, &slot);
+    if (s != RS_OK) return s;
     char* stage = ctx->pinned[slot];
     memcpy(stage, reqs.data(), sizeof(ReqDesc) * reqs.size());
     memcpy(stage + ds.reqs, items.data(), sizeof(AttnItem) * items.size());
@@ -950,7 +876,6 @@ rs_status prefill_enqueue(rs_ctx* ctx, const rs_layer_weights* w, int layer, rs_
     const bf16* xb = reinterpret_cast<const bf16*>(x);
     bf16* yb = reinterpret_cast<bf16*>(y);
     const int H = f.hidden, I = f.mlp_inter;
-    rs_status s;
     const StepTimer tm{ctx, st};
 
     rollback.armed = false;   // every host-side check has passed: from here on the call is launched
@@ -978,14 +903,7 @@ rs_status prefill_enqueue(rs_ctx* ctx, const rs_layer_weights* w, int layer, rs_
     else if (red.splits > MAX_PLANES) first_kernel(std::integral_constant<int, MAX_PLANES_FEW>{}, std::integral_constant<int, 256>{});
     else first_kernel_lanes(std::integral_constant<int, MAX_PLANES>{});
     RS_HIP(hipGetLastError());
-    if (use % RING_CHECKPOINT == RING_CHECKPOINT - 1) {
-        RS_HIP(hipEventRecord(ctx->slot_done[slot], st));
-        ctx->slot_recorded_at[slot] = use;
-    } else {
-        ctx->slot_recorded_at[slot] = -1;   // (what was recorded here belonged to the slot's previous use)
-    }
-    ctx->last_stream = st;
-    ctx->use_count = use + 1;
+    if ((s = ring_commit(ctx, st)) != RS_OK) return s;
     tm.end(RS_STEP_ROW_RMS);
     // qkv = rope( (x Wqkv'^T) / rms + b )
     tm.begin(RS_STEP_QKV_GEMM);
@@ -1037,7 +955,10 @@ rs_status prefill_enqueue(rs_ctx* ctx, const rs_layer_weights* w, int layer, rs_
     if ((s = gemm_residual(ctx, act, (const bf16*)w->w_down, r, 1, yb, 0, T, H, I, partial, L.planes, nullptr, nullptr, nullptr, st, pending_out)) != RS_OK) return s;
     tm.end(RS_STEP_DOWN_GEMM);
 
-    for (int i = 0; i < R; ++i) kvs[i]->len[layer] += lens[i];
+    for (int i = 0; i < R; ++i) {
+        kvs[i]->len[layer] += lens[i];
+        if (lens[i] > 0) kvs[i]->stale_tail[layer] = 0;   // (zeroed with the append)
+    }
     return RS_OK;
 }
 
@@ -1090,6 +1011,7 @@ rs_status rs_ctx_create(const rs_layer_cfg* cfg, rs_ctx** out) {
     auto cleanup = [&](rs_status s) { rs_ctx_destroy(c); return s; };
 
     c->slot_bytes = desc_sizes(c, f.max_tokens_per_call, f.max_requests).total + desc_sizes(c, f.max_tokens_per_call, f.max_requests).append;
+    c->slot_bytes = std::max(c->slot_bytes, attend_staging_bytes(f));
     int n_dev = 0;
     if (hipGetDeviceCount(&n_dev) != hipSuccess || n_dev <= 0) {
         (void)hipGetLastError();
@@ -1240,7 +1162,7 @@ rs_status rs_kv_alloc(rs_ctx* c, int n_layers, int capacity_tokens, void* dev_me
     kv->base = reinterpret_cast<char*>(dev_mem);
     kv->k_bytes = align_up((size_t)kv->cap * c->kv_dim * 2, 256);
     kv->layer_bytes = 2 * kv->k_bytes;
-    kv->len.assign(n_layers, 0);
+    kv->start_layers(n_layers);
     *out = kv;
     return RS_OK;
 }
@@ -1274,7 +1196,7 @@ rs_status rs_kv_alloc_fp8(rs_ctx* c, int n_layers, int capacity_tokens, float k_
     kv->base = reinterpret_cast<char*>(dev_mem);
     kv->k_bytes = align_up((size_t)kv->cap * c->kv_dim, 256);
     kv->layer_bytes = 2 * kv->k_bytes;
-    kv->len.assign(n_layers, 0);
+    kv->start_layers(n_layers);
     kv->fp8 = true;
     kv->k_scale = k_scale;
     kv->v_scale = v_scale;
@@ -1350,7 +1272,7 @@ static rs_status alloc_paged(rs_ctx* c, rs_kv_pool* pool, int n_layers, bool fp8
     kv->cap = 0;
     kv->base = nullptr;
     kv->k_bytes = kv->layer_bytes = 0;
-    kv->len.assign(n_layers, 0);
+    kv->start_layers(n_layers);
     kv->pool = pool;
     kv->fp8 = fp8;
     kv->k_scale = k_scale;
@@ -1385,6 +1307,7 @@ int rs_kv_capacity(const rs_kv* kv) {
 
 rs_status rs_kv_reset(rs_kv* kv) {
     if (!kv) return fail(RS_EINVAL, "kv is null");
+    for (int l = 0; l < kv->n_layers; ++l) kv->dropped_from(l, 0);
     std::fill(kv->len.begin(), kv->len.end(), 0);
     if (kv->paged())
         for (int l = 0; l < kv->n_layers; ++l) kv->give_back_pages(l, 0);
@@ -1395,6 +1318,7 @@ rs_status rs_kv_truncate(rs_kv* kv, int layer, int n_tokens) {
     if (!kv) return fail(RS_EINVAL, "kv is null");
     if (layer < 0 || layer >= kv->n_layers) return fail(RS_EINVAL, "layer %d out of range", layer);
     if (n_tokens < 0 || n_tokens > kv->len[layer]) return fail(RS_EINVAL, "n_tokens = %d outside [0, %d]", n_tokens, kv->len[layer]);
+    kv->dropped_from(layer, n_tokens);
     kv->len[layer] = n_tokens;
     if (kv->paged()) kv->give_back_pages(layer, n_tokens);
     return RS_OK;
@@ -1423,6 +1347,7 @@ rs_status rs_kv_import(rs_kv* kv, int layer, const void* k, const void* v, int n
         if (s != RS_OK) return s;
     }
     if (n_tokens == 0) {
+        kv->dropped_from(layer, 0);
         kv->len[layer] = 0;
         if (kv->paged()) kv->give_back_pages(layer, 0);
         return RS_OK;
@@ -1436,14 +1361,14 @@ rs_status rs_kv_import(rs_kv* kv, int layer, const void* k, const void* v, int n
     }
     if (kv->fp8) {
         const rs_status s = fp8_import(kv, layer, (const bf16*)k, (const bf16*)v, n_tokens, st);
-        if (s == RS_OK) kv->len[layer] = n_tokens;
+        if (s == RS_OK) imported(kv, layer, n_tokens);
         return s;
     }
     for_each_kv_window(kv, layer, n_tokens, [&](const ReqDesc& rq, const KVPageWindow& win, int b0, int t0, int nt) {
         launch_import<bf16>(kv->ctx, rq, Fp8CacheDesc{}, win, b0, (const bf16*)k, (const bf16*)v, t0, nt, st);
     });
     RS_HIP(hipGetLastError());
-    kv->len[layer] = n_tokens;
+    imported(kv, layer, n_tokens);
     return RS_OK;
 }
 
@@ -1465,6 +1390,7 @@ rs_status rs_kv_import_codes(rs_kv* kv, int layer, const void* k_codes, const vo
         if (s != RS_OK) return s;
     }
     if (n_tokens == 0) {
+        kv->dropped_from(layer, 0);
         kv->len[layer] = 0;
         if (kv->paged()) kv->give_back_pages(layer, 0);
         return RS_OK;
@@ -1476,7 +1402,7 @@ rs_status rs_kv_import_codes(rs_kv* kv, int layer, const void* k_codes, const vo
         kv->give_back_pages(layer, n_tokens);
     }
     const rs_status s = fp8_import(kv, layer, (const uint8_t*)k_codes, (const uint8_t*)v_codes, n_tokens, reinterpret_cast<hipStream_t>(stream));
-    if (s == RS_OK) kv->len[layer] = n_tokens;
+    if (s == RS_OK) imported(kv, layer, n_tokens);
     return s;
 }
 
