@@ -4,10 +4,11 @@
 //   out[row] = sum_k w_k value_k / sum_k w_k,   w_k = 2^(scale log2e q . key_k - m),  m a reference that tracks the maximum
 //
 // Bound by the bytes of the keys and values: a tile of 64 keys is 32 KB (d = 128, bfloat16), and the rows that share it - the g
-// query heads of a KV head, times the tokens - give it 16 MFMAs of 16 clocks per 16 rows and product.  So nothing is shared
-// between wavefronts and nothing goes through LDS: each wavefront owns whole tiles, loads a tile straight into the MFMA operand
-// layout (16 rows x 64 bytes per instruction; the tile is contiguous, so every line is used whole), and the next tile's keys are
-// under way while the softmax runs, its values while the next scores are formed: up to 32 KB in flight per wavefront.
+// query heads of a KV head, times the tokens - give it 16 MFMAs of 16 clocks per 16 rows and product.  So wavefronts share no tiles: each
+// streams its own through its own LDS, by DMA, without barriers, in units of 8 KB of keys and 8 KB of values: the next unit's keys
+// are under way as soon as this one's are in registers, its values likewise.  (Loads straight into the MFMA operand layout, where
+// neighbouring lanes are different keys, need no LDS, but the address unit then takes 64 clocks for a load of a KB instead of 16: a
+// compute unit gets 16 bytes per clock, whatever the cache they come from.)
 //
 // As in the chunk kernel (attention.h) the transposed products keep a query in one lane (lane & 15):
 //   S^T[key, query] = K Q^T,   O^T[d, query] = V^T P^T   with v_mfma_f32_16x16x32_bf16
@@ -15,8 +16,10 @@
 // consecutive keys that it has to feed to the second product.  8-bit tiles are loaded 16 codes at a time (the keys' order
 // changes with it) and become bfloat16, exactly, in registers; their scales go into the softmax's scale and the output.
 //
-// Work item = (request, KV head, block of 16 NB stacked rows, part of the key range).  Four wavefronts take the item's tiles in
-// turn and meet in LDS once; parts leave unnormalised sums, references and row sums in slots that few_merge_kernel joins.
+// Work item = (request, KV head, part of the key range), with up to 64 stacked rows.  A wavefront has 16 of them: with up to 16 rows the four
+// wavefronts of a workgroup take the item's tiles in turn, with up to 32 two pairs do, with more each takes every tile (the others'
+// loads of it hit in the caches; a wavefront with more rows of its own would have no registers for loads in flight).  They meet in LDS
+// once; parts leave unnormalised sums, references and row sums in slots that few_merge_kernel joins.
 #pragma once
 #include "attention.h"
 #include "common.h"
@@ -90,257 +93,339 @@ struct FewArgs {
     int n_blocks, list_parts;
 };
 
+#define RS_UNIT __device__ __forceinline__
 constexpr int FEW_WAVES = 4;
 constexpr int FEW_MAX_PARTS = 64;
 constexpr float FEW_HEADROOM = 8.0f;   // the reference moves when a score exceeds it by this many powers of two
 
-template <int D, int NB>
-struct FewSlot {   // [16 NB rows][D] sums, then references, then row sums
-    static constexpr size_t FLOATS = (size_t)16 * NB * (D + 2);
+// Blocks of 16 rows that `rows` of them are handled as: 1, 2 or 4.
+__host__ __device__ inline int few_row_blocks(int rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
+
+template <int D>
+struct FewSlot {   // of a part and 16 rows: [16][D] sums, then references, then row sums
+    static constexpr size_t FLOATS = (size_t)16 * (D + 2);
 };
 
-template <int D, bool FP8, int NB, bool LIST, bool INLINE>
-__global__ __launch_bounds__(64 * FEW_WAVES, NB == 1 ? 2 : 1) void attend_few_kernel(FewArgs a, std::conditional_t<INLINE, InlineTable, NoTable> tab) {
-    constexpr int KS = D / 32, DT = D / 16, RB = FP8 ? D : 2 * D;
-    constexpr int KL = FP8 ? 4 * (D / 64) : 4 * KS, VL = FP8 ? DT : 2 * DT;   // 16-byte loads per lane of a tile's keys, values
-    __shared__ __attribute__((aligned(16))) float red[FEW_WAVES][16][D + 4];
-    __shared__ float m_sh[FEW_WAVES][16 * NB], l_sh[FEW_WAVES][16 * NB];
+// An item's rows, and where they are in q and out.
+template <bool LIST>
+struct FewRows {
+    int row0, P, kvh, g, tok0, rows;   // (LIST: the g heads of one token)
+    __device__ __forceinline__ int token(int i) const { return LIST ? tok0 : i / g; }
+    __device__ __forceinline__ int head(int i) const { return kvh * g + (LIST ? i : i % g); }
+};
+
+// A wavefront's unit of work: KEYS keys of a tile, their K rows and V^T columns BYTES each in LDS.  16-byte chunks sit at places of their row
+// that make the 8 lanes of a read, which are 8 keys or features of one chunk, meet different banks; a load instruction fills 1 KB of LDS
+// linearly by lane, each lane fetching the chunk that belongs in its place.
+template <int D, bool FP8>
+struct FewUnit {
+    static constexpr int EL = FP8 ? 1 : 2;
+    static constexpr int TILE = 64 * D * EL;                          // bytes of a tile
+    static constexpr int PER_TILE = TILE > 8192 ? TILE / 8192 : 1;
+    static constexpr int KEYS = 64 / PER_TILE, BYTES = TILE / PER_TILE, LOADS = BYTES / 1024;
+    static constexpr int K_ROW = D * EL, K_CHUNKS = K_ROW / 16;       // a key's bytes, chunks
+    static constexpr int K_READS = K_CHUNKS / 4;                      // 16-byte reads of a lane per 16 keys
+    static constexpr int V_TILE_ROW = 64 * EL, V_ROW = KEYS * EL;     // a feature's bytes in the tile, in the unit
+    static constexpr int V_CHUNKS = V_ROW / 64;                       // 16-byte reads of a lane per 16 features
+    // Key of MFMA row i of sub-tile t: the scores a lane ends up with - rows 4 c .. 4 c + 3 of every sub-tile - are the keys it multiplies
+    // with values, consecutive ones: 8 of every 32, or with 8-bit values, which come 16 to a chunk, 16 of 64.
+    RS_UNIT static int key_of(int t, int i) {
+        return FP8 ? (i >> 2) * 16 + t * 4 + (i & 3) : (t >> 1) * 32 + (i >> 2) * 8 + (t & 1) * 4 + (i & 3);
+    }
+    RS_UNIT static int k_swizzle(int key) {   // of a key's chunks: from its MFMA row
+        const int i = (key & 3) | ((FP8 ? key >> 4 : key >> 3) & 3) << 2;
+        return K_CHUNKS == 16 ? i : K_CHUNKS == 8 ? i & 7 : (i >> 1) & 3;
+    }
+    RS_UNIT static int v_swizzle(int feature) { return V_ROW == 128 ? feature & 7 : (feature >> 1) & 3; }
+    RS_UNIT static uint32_t k_place(int key, int chunk) { return (uint32_t)(key * K_ROW + (chunk ^ k_swizzle(key)) * 16); }
+    RS_UNIT static uint32_t v_place(int feature, int chunk) { return (uint32_t)(feature * V_ROW + (chunk ^ v_swizzle(feature)) * 16); }
+    // bytes from a lane's chunks of sub-tile 0 to those of sub-tile t (the swizzle is the MFMA row's: the same)
+    RS_UNIT static constexpr int k_step(int t) { return (FP8 ? t * 4 : (t >> 1) * 32 + (t & 1) * 4) * K_ROW; }
+    // where in the tile the chunk that belongs at place p of the unit is
+    RS_UNIT static uint32_t k_source(int p) {
+        const int key = p / K_CHUNKS;
+        return (uint32_t)(key * K_ROW + (p % K_CHUNKS ^ k_swizzle(key)) * 16);
+    }
+    RS_UNIT static uint32_t v_source(int p) {
+        const int f = p / (V_ROW / 16);
+        return (uint32_t)(f * V_TILE_ROW + (p % (V_ROW / 16) ^ v_swizzle(f)) * 16);
+    }
+    // load instructions after which the keys' sources repeat, as many keys further on
+    static constexpr int K_PATTERNS = (FP8 ? 64 : 32) * K_ROW / 1024 < LOADS ? (FP8 ? 64 : 32) * K_ROW / 1024 : LOADS;
+    // (values: every one; a KB is 8 or 16 features)
+};
+
+template <int D, bool FP8, bool LIST, bool INLINE>
+__global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a, std::conditional_t<INLINE, InlineTable, NoTable> tab) {
+    typedef FewUnit<D, FP8> U;
+    constexpr int KS = D / 32, DT = D / 16, NT = U::KEYS / 16;
+    __shared__ __attribute__((aligned(16))) char lds[FEW_WAVES * 2 * U::BYTES];   // each wavefront's keys and values, in the end its sums
+    __shared__ float m_sh[FEW_WAVES][16], l_sh[FEW_WAVES][16];
     const uint32_t* const table = table_of<INLINE>(tab, a.table);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, c = lane >> 4;
 
     // ---- which rows, which tiles
-    int req, kvh, part, parts, row_first, rows_here, tok0, unit;
+    FewRows<LIST> rows;
+    int req, part, parts, unit, n;   // n: tiles, or blocks of the list
+    const int* list = nullptr;
+    rows.g = a.g;
     if constexpr (LIST) {
         int id = blockIdx.x;
-        kvh = id % a.hkv;
+        rows.kvh = id % a.hkv;
         id /= a.hkv;
         parts = a.list_parts;
         part = id % parts;
         const int row = id / parts;
         req = request_of(table, a.n_req, (uint32_t)row);
-        unit = row * a.hkv + kvh;
-        row_first = row;
-        rows_here = a.g;
+        unit = row * a.hkv + rows.kvh;
+        rows.tok0 = row;
+        rows.rows = a.g;
     } else {
         req = request_of(table, a.n_req, blockIdx.x);
-        unit = row_first = rows_here = part = parts = kvh = 0;
+        unit = part = parts = 0;
     }
     const FewReq rq = reinterpret_cast<const FewReq*>(table + table_reqs_at(a.n_req))[req];
-    int kb0, kb1;
-    const int* list = nullptr;
+    rows.row0 = rq.row0;
+    rows.P = rq.P;
     if constexpr (LIST) {
-        tok0 = row_first - rq.row0;
+        rows.tok0 -= rq.row0;
         list = a.chosen + (size_t)unit * a.n_blocks;
-        const int n = min(a.n_blocks, (rq.P + tok0) / 64 + 1);   // (the list ends there)
-        kb0 = (int)((long)n * part / parts);
-        kb1 = (int)((long)n * (part + 1) / parts);
+        n = min(a.n_blocks, (rq.P + rows.tok0) / 64 + 1);   // (the list ends there)
     } else {
-        int id = (int)(blockIdx.x - table[req]);
+        const int id = (int)(blockIdx.x - table[req]);
         parts = rq.parts;
-        kvh = id % a.hkv;
-        id /= a.hkv;
-        part = id % parts;
-        const int rb = id / parts;
-        unit = rb * a.hkv + kvh;
-        row_first = rb * 16 * NB;                                 // of the request's T g stacked rows
-        rows_here = min(16 * NB, rq.T * a.g - row_first);
-        tok0 = row_first / a.g;
-        const int n = (rq.P + (row_first + rows_here - 1) / a.g) / 64 + 1;
-        kb0 = (int)((long)n * part / parts);
-        kb1 = (int)((long)n * (part + 1) / parts);
+        unit = rows.kvh = id % a.hkv;
+        part = id / a.hkv;
+        rows.tok0 = 0;
+        rows.rows = rq.T * a.g;
+        n = (rq.P + rq.T - 1) / 64 + 1;
     }
-    const auto token_of = [&](int col) RS_INLINE { return LIST ? tok0 : (row_first + col) / a.g; };
-    const auto head_of = [&](int col) RS_INLINE { return kvh * a.g + (LIST ? col : (row_first + col) % a.g); };
+    const int kb0 = (int)((long)n * part / parts), kb1 = (int)((long)n * (part + 1) / parts);
+    const int rbn = few_row_blocks(rows.rows), rb = wave & (rbn - 1), step = FEW_WAVES / rbn;
     const auto tile_at = [&](int i, global_bytes& kt, global_bytes& vt, int& block) RS_INLINE {
         block = i;
-        if constexpr (LIST) {
-            block = list[i];
-            if (block < 0) return false;
-        }
+        if constexpr (LIST) block = list[i];
         const uint64_t index = rq.pages == CONTIGUOUS ? (uint32_t)block : table[rq.pages + block];
-        const uint64_t off = (uint64_t)kvh * rq.head_bytes + index * rq.block_bytes;
+        const uint64_t off = (uint64_t)rows.kvh * rq.head_bytes + index * rq.block_bytes;
         kt = (global_bytes)(rq.k + off);
         vt = (global_bytes)(rq.v + off);
-        return true;
     };
 
     // ---- queries
-    bf16x8 qf[NB][KS];
-    int qpos[NB];
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-        const int col = min(nb * 16 + r, rows_here - 1);   // (rows past the end repeat the last one and are not stored)
-        const int tok = token_of(col);
-        qpos[nb] = rq.P + tok;
-        const bf16* p = a.q + (size_t)(rq.row0 + tok) * a.ld_q + head_of(col) * D;
+    bf16x8 qf[KS];
+    int qpos;
+    {
+        const int i = min(rb * 16 + r, rows.rows - 1);   // (rows past the end repeat the last one and are not stored)
+        qpos = rq.P + rows.token(i);
+        const bf16* p = a.q + (size_t)(rq.row0 + rows.token(i)) * a.ld_q + rows.head(i) * D;
 #pragma unroll
         for (int kk = 0; kk < KS; ++kk)
-            qf[nb][kk] = *reinterpret_cast<const bf16x8*>(p + (FP8 ? (kk >> 1) * 64 + c * 16 + (kk & 1) * 8 : kk * 32 + c * 8));
+            qf[kk] = *reinterpret_cast<const bf16x8*>(p + (FP8 ? (kk >> 1) * 64 + c * 16 + (kk & 1) * 8 : kk * 32 + c * 8));
     }
-    const int seen_by_all = rq.P + tok0;   // every row of the item sees the keys up to here
+    const int seen_by_all = rq.P + rows.tok0;   // every row of the item sees the keys up to here
     const float sc = FP8 ? a.scale_log2e * rq.k_scale : a.scale_log2e;
 
-    f32x4 acc[NB][DT];
-    float m[NB], l[NB];
+    f32x4 acc[DT];
+    float m = -INFINITY, l = 0.0f;
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-        m[nb] = -INFINITY;
-        l[nb] = 0.0f;
+    for (int dt = 0; dt < DT; ++dt) acc[dt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    // ---- this wavefront's tiles kb0 + wave / rbn, + step, ...; their places (page or block) in a register, a lane each, 64 at a time
+    const int first = kb0 + wave / rbn, tiles = rb * 16 < rows.rows && first < kb1 ? (kb1 - first + step - 1) / step : 0;
+    int place = 0, number = 0;
+    const auto look_up = [&](int j0) RS_INLINE {   // of tiles j0 .. j0 + 63
+        const int i = min(first + (j0 + lane) * step, kb1 - 1);
+        number = LIST ? list[i] : i;
+        place = rq.pages == CONTIGUOUS ? number : (int)table[rq.pages + number];
+    };
+    typedef __attribute__((address_space(3))) void* lds_ptr;
+    char* const k_mine = lds + wave * 2 * U::BYTES;
+    char* const v_mine = k_mine + U::BYTES;
+    const uint64_t k_head = rq.k + (uint64_t)rows.kvh * rq.head_bytes, v_head = rq.v + (uint64_t)rows.kvh * rq.head_bytes;
+    uint32_t k_src[8];   // where a lane's 16 bytes of a load instruction come from (U::K_PATTERNS of them; values: one)
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) acc[nb][dt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    }
-    const uint32_t k_off = (uint32_t)(((r >> 2) * (FP8 ? 16 : 8) + (r & 3)) * RB + c * 16);
-    const uint32_t v_off = (uint32_t)(r * (FP8 ? 64 : 128) + c * 16);
-    uint4 kf[KL], vf[VL];
-    const auto load_k = [&](global_bytes kt) RS_INLINE {
+    for (int i = 0; i < U::K_PATTERNS; ++i) k_src[i] = U::k_source(i * 64 + lane);
+    const uint32_t v_src = U::v_source(lane);
+    const auto tile_of = [&](uint64_t head, int j) RS_INLINE {
+        return (void*)(head + (uint64_t)(uint32_t)__builtin_amdgcn_readlane(place, j & 63) * rq.block_bytes);
+    };
+    const auto fetch_k = [&](int u) RS_INLINE {
+        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(tile_of(k_head, u / U::PER_TILE), 0, U::TILE, 0x00020000);
+        const int soff = u % U::PER_TILE * U::BYTES;   // (keys are rows: a unit is contiguous)
 #pragma unroll
-        for (int i = 0; i < KL; ++i) {
-            constexpr int PER = KL / 4;   // loads of a sub-tile of 16 keys
-            const int t = i / PER, kk = i % PER;
-            const int key = FP8 ? t * 4 : (t >> 1) * 32 + (t & 1) * 4;
-            kf[i] = ld_tile_16(kt + k_off + (key * RB + kk * 64));
+        for (int i = 0; i < U::LOADS; ++i) {
+            const uint32_t from = k_src[i % U::K_PATTERNS];   // (named: template-dependent arguments of the builtin break the host-side stub)
+            const int further = soff + i / U::K_PATTERNS * U::K_PATTERNS * 1024;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)(uintptr_t)(uint32_t)(uintptr_t)(k_mine + i * 1024), 16, from, further, 0, 0);
         }
     };
-    const auto load_v = [&](global_bytes vt) RS_INLINE {
+    const auto fetch_v = [&](int u) RS_INLINE {
+        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(tile_of(v_head, u / U::PER_TILE), 0, U::TILE, 0x00020000);
+        const int soff = u % U::PER_TILE * U::V_ROW;   // (of every feature's row of 64 keys, the unit's part)
 #pragma unroll
-        for (int i = 0; i < VL; ++i) vf[i] = ld_tile_16(vt + v_off + (FP8 ? i * 16 * 64 : (i >> 1) * 16 * 128 + (i & 1) * 64));
+        for (int i = 0; i < U::LOADS; ++i) {
+            const uint32_t from = v_src;   // (named: template-dependent arguments of the builtin break the host-side stub)
+            const int further = soff + i * 1024 / U::V_ROW * U::V_TILE_ROW;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)(uintptr_t)(uint32_t)(uintptr_t)(v_mine + i * 1024), 16, from, further, 0, 0);
+        }
     };
-
-    // ---- tiles kb0 + wave, + 4, ...
-    global_bytes kt = nullptr, vt = nullptr;
-    int block = 0, kb = kb0 + wave;
-    bool have = kb < kb1 && tile_at(kb, kt, vt, block);
-    if (have) {
-        load_k(kt);
-        load_v(vt);
-    }
-    while (have) {
-        f32x4 s[NB][4];
+    // (the compiler does not see LDS written by DMA, nor may it move a refill above the reads of what it overwrites)
+    const auto wait_loads = [&](bool others) RS_INLINE {   // others: U::LOADS younger ones may be in flight
+        __builtin_amdgcn_sched_barrier(0);
+        if (others) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(U::LOADS) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    const auto reads_done = [&]() RS_INLINE {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    uint32_t k_at[4], v_at[2];   // a lane's fragments: sub-tile 0, features 0 .. 15
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+    for (int i = 0; i < U::K_READS; ++i) k_at[i] = U::k_place(U::key_of(0, r), i * 4 + c);
+#pragma unroll
+    for (int i = 0; i < U::V_CHUNKS; ++i) v_at[i] = U::v_place(r, i * 4 + c);
+
+    const int units = tiles * U::PER_TILE;
+    if (units > 0) {
+        look_up(0);
+        fetch_k(0);
+        fetch_v(0);
+    }
+    int block = 0;
+    for (int u = 0; u < units; ++u) {
+        if (u % U::PER_TILE == 0) block = __builtin_amdgcn_readlane(number, u / U::PER_TILE & 63);
+        const int key0 = block * 64 + u % U::PER_TILE * U::KEYS;
+        const bool more = u + 1 < units;
+        // (places are needed up to one unit ahead)
+        if (more && (u + 1) % (64 * U::PER_TILE) == 0) look_up((u + 1) / U::PER_TILE);
+        wait_loads(true);
+        uint4 kf[NT * U::K_READS];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < U::K_READS; ++i)
+                kf[t * U::K_READS + i] = *reinterpret_cast<const uint4*>(k_mine + k_at[i] + U::k_step(t));
+        reads_done();
+        if (more) fetch_k(u + 1);
+        f32x4 s[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int kk = 0; kk < KS; ++kk) {
                 bf16x8 kfrag;
                 if constexpr (FP8) {
-                    const uint4 w = kf[t * (KS / 2) + (kk >> 1)];
+                    const uint4 w = kf[t * U::K_READS + (kk >> 1)];
                     kfrag = (kk & 1) ? bf16x8_of_codes(w.z, w.w) : bf16x8_of_codes(w.x, w.y);
                 } else {
-                    kfrag = as_bf16x8(kf[t * KS + kk]);
+                    kfrag = as_bf16x8(kf[t * U::K_READS + kk]);
                 }
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb)
-                    s[nb][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kfrag, qf[nb][kk], kk == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : s[nb][t], 0, 0, 0);
+                s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kfrag, qf[kk], kk == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : s[t], 0, 0, 0);
             }
-        const int key0 = block * 64;
-        global_bytes vt_next = nullptr;
-        kb += FEW_WAVES;
-        have = kb < kb1 && tile_at(kb, kt, vt_next, block);
-        if (have) load_k(kt);
-        bf16x8 pf[NB][2];
+        if (key0 + U::KEYS - 1 > seen_by_all) {
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-            if (key0 + 63 > seen_by_all) {
+            for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int t = 0; t < 4; ++t)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int key = key0 + (FP8 ? c * 16 + t * 4 : (t >> 1) * 32 + c * 8 + (t & 1) * 4) + e;
-                        s[nb][t][e] = key <= qpos[nb] ? s[nb][t][e] : -INFINITY;
-                    }
-            }
-            float mx = s[nb][0][0];
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[nb][t][e]);
-            mx = fmaxf(mx, __shfl_xor(mx, 16, WAVE));
-            mx = fmaxf(mx, __shfl_xor(mx, 32, WAVE)) * sc;
-            const bool move = mx > m[nb] + FEW_HEADROOM;   // (at first m is minus infinity)
-            if (__builtin_amdgcn_ballot_w64(move)) {
-                const float m_new = move ? mx : m[nb];
-                const float alpha = m[nb] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[nb] - m_new);
-                m[nb] = m_new;
-                l[nb] *= alpha;
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[nb][dt][e] *= alpha;
-            }
-            const float ref = m[nb] == -INFINITY ? 0.0f : m[nb];
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[nb][t][e], sc, -ref));
-                    l[nb] += p;
-                    pf[nb][t >> 1][(t & 1) * 4 + e] = f32_to_bf16(p);
-                }
+                for (int e = 0; e < 4; ++e) s[t][e] = key0 + U::key_of(t, c * 4 + e) <= qpos ? s[t][e] : -INFINITY;
         }
+        float mx = s[0][0];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[t][e]);
+        mx = fmaxf(mx, __shfl_xor(mx, 16, WAVE));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, WAVE)) * sc;
+        const bool move = mx > m + FEW_HEADROOM;   // (at first m is minus infinity)
+        if (__builtin_amdgcn_ballot_w64(move)) {
+            const float m_new = move ? mx : m;
+            const float alpha = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - m_new);
+            m = m_new;
+            l *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[dt][e] *= alpha;
+        }
+        const float ref = m == -INFINITY ? 0.0f : m;
+        bf16x8 pf[NT / 2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e], sc, -ref));
+                l += p;
+                pf[t >> 1][(t & 1) * 4 + e] = f32_to_bf16(p);
+            }
+        wait_loads(more);
+        uint4 vf[DT * U::V_CHUNKS];
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-            for (int s2 = 0; s2 < 2; ++s2) {
+            for (int i = 0; i < U::V_CHUNKS; ++i)
+                vf[dt * U::V_CHUNKS + i] = *reinterpret_cast<const uint4*>(v_mine + v_at[i] + dt * 16 * U::V_ROW);
+        reads_done();
+        if (more) fetch_v(u + 1);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int s2 = 0; s2 < NT / 2; ++s2) {
                 bf16x8 vfrag;
                 if constexpr (FP8) vfrag = s2 ? bf16x8_of_codes(vf[dt].z, vf[dt].w) : bf16x8_of_codes(vf[dt].x, vf[dt].y);
-                else vfrag = as_bf16x8(vf[dt * 2 + s2]);
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) acc[nb][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vfrag, pf[nb][s2], acc[nb][dt], 0, 0, 0);
+                else vfrag = as_bf16x8(vf[dt * U::V_CHUNKS + s2]);
+                acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vfrag, pf[s2], acc[dt], 0, 0, 0);
             }
-        if (have) load_v(vt_next);
     }
 
-    // ---- the four wavefronts meet
+    static_assert(16 * (D + 4) * 4 <= 2 * U::BYTES, "a wavefront's sums fit where its keys and values were");
+    const auto sums_of = [&](int w, int row) RS_INLINE { return reinterpret_cast<float*>(lds + w * 2 * U::BYTES) + row * (D + 4); };
+    // ---- the wavefronts of the same rows meet: each brings its sums to the largest reference among them
+    l += __shfl_xor(l, 16, WAVE);
+    l += __shfl_xor(l, 32, WAVE);
+    if (c == 0) {
+        m_sh[wave][r] = m;
+        l_sh[wave][r] = l;
+    }
+    __syncthreads();
+    float big = m;
+    for (int w = rb; w < FEW_WAVES; w += rbn) big = fmaxf(big, m_sh[w][r]);
+    const float weight = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - big);
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-        l[nb] += __shfl_xor(l[nb], 16, WAVE);
-        l[nb] += __shfl_xor(l[nb], 32, WAVE);
-        if (c == 0) {
-            m_sh[wave][nb * 16 + r] = m[nb];
-            l_sh[wave][nb * 16 + r] = l[nb];
-        }
+    for (int dt = 0; dt < DT; ++dt) {
+        f32x4 o = acc[dt];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] *= weight;
+        *reinterpret_cast<f32x4*>(sums_of(wave, r) + dt * 16 + c * 4) = o;
     }
     __syncthreads();
     constexpr int PER = D / 16;   // features of a thread
-    float* const slot = a.slots + (size_t)(rq.slot0 + unit * parts + part) * FewSlot<D, NB>::FLOATS;
+    const int row = threadIdx.x >> 4, f0 = (threadIdx.x & 15) * PER;
+    for (int b = 0; b < rbn && b * 16 < rows.rows; ++b) {
+        float M = -INFINITY, L = 0.0f, o[PER] = {};
+        for (int w = b; w < FEW_WAVES; w += rbn) M = fmaxf(M, m_sh[w][row]);
+        for (int w = b; w < FEW_WAVES; w += rbn) {
+            L += l_sh[w][row] == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(m_sh[w][row] - M) * l_sh[w][row];
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-        float big = m_sh[0][nb * 16 + r];
-#pragma unroll
-        for (int w = 1; w < FEW_WAVES; ++w) big = fmaxf(big, m_sh[w][nb * 16 + r]);
-        const float weight = m[nb] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[nb] - big);
-        if (nb > 0) __syncthreads();   // (the last rows' readers are done)
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-            f32x4 o = acc[nb][dt];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] *= weight;
-            *reinterpret_cast<f32x4*>(&red[wave][r][dt * 16 + c * 4]) = o;
+            for (int j = 0; j < PER; ++j) o[j] += sums_of(w, row)[f0 + j];
         }
-        __syncthreads();
-        const int row = threadIdx.x >> 4, f0 = (threadIdx.x & 15) * PER, col = nb * 16 + row;
-        float M = m_sh[0][col], L = 0.0f, o[PER];
-#pragma unroll
-        for (int w = 1; w < FEW_WAVES; ++w) M = fmaxf(M, m_sh[w][col]);
-#pragma unroll
-        for (int w = 0; w < FEW_WAVES; ++w) L += l_sh[w][col] == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(m_sh[w][col] - M) * l_sh[w][col];
         bool bad = !(fabsf(L) <= 3.402823466e38f);
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
-            o[j] = ((red[0][row][f0 + j] + red[1][row][f0 + j]) + (red[2][row][f0 + j] + red[3][row][f0 + j])) * (FP8 ? rq.v_scale : 1.0f);
+            if constexpr (FP8) o[j] *= rq.v_scale;
             bad |= !(fabsf(o[j]) <= 3.402823466e38f);
         }
-        const bool live = col < rows_here;
-        const int col_c = min(col, rows_here - 1);
-        bf16* const op = a.out + (size_t)(rq.row0 + token_of(col_c)) * a.ld_out + head_of(col_c) * D;
+        const int i = b * 16 + row;
+        const bool live = i < rows.rows;
+        const int ic = min(i, rows.rows - 1);
+        bf16* const op = a.out + (size_t)(rq.row0 + rows.token(ic)) * a.ld_out + rows.head(ic) * D;
+        float* const slot = a.slots + (size_t)(rq.slot0 + (unit * parts + part) * rbn + b) * FewSlot<D>::FLOATS;
         const unsigned long long any = __builtin_amdgcn_ballot_w64(bad && live);
         const bool again = ((any >> (lane & 48)) & 0xffffu) != 0;   // (a row's sixteen threads are neighbours)
         if (!again && parts > 1) {
 #pragma unroll
-            for (int j = 0; j < PER; j += 4) *reinterpret_cast<f32x4*>(slot + (size_t)col * D + f0 + j) = f32x4{o[j], o[j + 1], o[j + 2], o[j + 3]};
+            for (int j = 0; j < PER; j += 4) *reinterpret_cast<f32x4*>(slot + (size_t)row * D + f0 + j) = f32x4{o[j], o[j + 1], o[j + 2], o[j + 3]};
             if (f0 == 0) {
-                slot[(size_t)16 * NB * D + col] = M;
-                slot[(size_t)16 * NB * (D + 1) + col] = L;
+                slot[(size_t)16 * D + row] = M;
+                slot[(size_t)16 * (D + 1) + row] = L;
             }
         } else if (!again && live) {
             const float inv = 1.0f / L;
@@ -357,100 +442,103 @@ __global__ __launch_bounds__(64 * FEW_WAVES, NB == 1 ? 2 : 1) void attend_few_ke
             }
         }
         if (__builtin_expect(any != 0, 0)) {
-            for (int i = 0; i < 4; ++i) {   // the wavefront's four rows
-                if (((any >> (16 * i)) & 0xffffu) == 0) continue;
-                const int bc = nb * 16 + wave * 4 + i, tok = token_of(bc), head = head_of(bc);
+            for (int k = 0; k < 4; ++k) {   // the wavefront's four rows
+                if (((any >> (16 * k)) & 0xffffu) == 0) continue;
+                const int bi = b * 16 + wave * 4 + k, tok = rows.token(bi), head = rows.head(bi);
                 float em, el, eo[D / 64];
                 exact_row<D, FP8>(a.q + (size_t)(rq.row0 + tok) * a.ld_q + head * D, sc, rq.P + tok, kb0, kb1, tile_at, em, el, eo);
                 bf16* const bp = a.out + (size_t)(rq.row0 + tok) * a.ld_out + head * D;
 #pragma unroll
                 for (int j = 0; j < D / 64; ++j) {
                     const float v = eo[j] * (FP8 ? rq.v_scale : 1.0f);
-                    if (parts > 1) slot[(size_t)bc * D + lane + 64 * j] = v;
+                    if (parts > 1) slot[(size_t)(wave * 4 + k) * D + lane + 64 * j] = v;
                     else bp[lane + 64 * j] = f32_to_bf16(v / el);
                 }
                 if (parts > 1 && lane == 0) {
-                    slot[(size_t)16 * NB * D + bc] = em;
-                    slot[(size_t)16 * NB * (D + 1) + bc] = el;
+                    slot[(size_t)16 * D + wave * 4 + k] = em;
+                    slot[(size_t)16 * (D + 1) + wave * 4 + k] = el;
                 }
             }
         }
     }
 }
 
-// Joins the parts of an item:  M = max_p m_p,  out = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p.  One workgroup per item and 32
+// Joins the parts of 16 rows:  M = max_p m_p,  out = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p.  One workgroup per 16 rows and 32
 // features, a quarter of the parts per 64 threads (16 rows x 4 chunks of 8 features).
-template <int D, int NB, bool LIST, bool INLINE>
+template <int D, bool LIST, bool INLINE>
 __global__ __launch_bounds__(256) void few_merge_kernel(FewArgs a, std::conditional_t<INLINE, InlineTable, NoTable> tab) {
     constexpr int MAXP = FEW_MAX_PARTS / 4;
     __shared__ float m_sh[4][16];
     __shared__ float red[4][64][9];
     const uint32_t* const table = table_of<INLINE>(tab, a.table);
-    int req, parts, unit, kvh, row_first, rows_here;
+    FewRows<LIST> rows;
+    rows.g = a.g;
+    int req, parts, unit, b = 0;
     if constexpr (LIST) {
-        unit = blockIdx.x;
-        kvh = unit % a.hkv;
-        row_first = unit / a.hkv;
-        req = request_of(table, a.n_req, (uint32_t)row_first);
+        const int rbn = few_row_blocks(a.g);
+        b = blockIdx.x % rbn;
+        unit = blockIdx.x / rbn;
+        rows.kvh = unit % a.hkv;
+        rows.tok0 = unit / a.hkv;
+        req = request_of(table, a.n_req, (uint32_t)rows.tok0);
     } else {
         req = request_of(table + table_units_at(a.n_req), a.n_req, blockIdx.x);
-        unit = (int)(blockIdx.x - table[table_units_at(a.n_req) + req]);
-        row_first = kvh = 0;
+        unit = 0;
     }
     const FewReq rq = reinterpret_cast<const FewReq*>(table + table_reqs_at(a.n_req))[req];
     parts = LIST ? a.list_parts : rq.parts;
     if (parts <= 1) return;
     if constexpr (LIST) {
-        rows_here = a.g;
+        rows.tok0 -= rq.row0;
+        rows.rows = a.g;
     } else {
-        kvh = unit % a.hkv;
-        row_first = unit / a.hkv * 16 * NB;
-        rows_here = min(16 * NB, rq.T * a.g - row_first);
+        rows.tok0 = 0;
+        rows.rows = rq.T * a.g;
+        const int id = (int)(blockIdx.x - table[table_units_at(a.n_req) + req]);
+        unit = rows.kvh = id % a.hkv;
+        b = id / a.hkv;
     }
-    const int group = threadIdx.x >> 6, row = (threadIdx.x & 63) >> 2, f0 = blockIdx.y * 32 + (threadIdx.x & 3) * 8;
-    for (int nb = 0; nb < NB; ++nb) {
-        const int col = nb * 16 + row;
-        if (nb * 16 >= rows_here) return;   // (the whole workgroup)
-        const float* const base = a.slots + (size_t)(rq.slot0 + unit * parts) * FewSlot<D, NB>::FLOATS;
-        float mp[MAXP], M = -INFINITY, L = 0.0f, o[8] = {};
+    const int rbn = few_row_blocks(rows.rows);
+    if (b * 16 >= rows.rows) return;
+    const int group = threadIdx.x >> 6, row = (threadIdx.x & 63) >> 2, f0 = blockIdx.y * 32 + (threadIdx.x & 3) * 8, i = b * 16 + row;
+    const float* const base = a.slots + (size_t)(rq.slot0 + unit * parts * rbn + b) * FewSlot<D>::FLOATS;
+    const size_t next = (size_t)rbn * FewSlot<D>::FLOATS;
+    float mp[MAXP], M = -INFINITY, L = 0.0f, o[8] = {};
 #pragma unroll
-        for (int i = 0; i < MAXP; ++i) {
-            const int p = i * 4 + group;
-            mp[i] = p < parts ? base[(size_t)p * FewSlot<D, NB>::FLOATS + (size_t)16 * NB * D + col] : -INFINITY;
-            M = fmaxf(M, mp[i]);
+    for (int k = 0; k < MAXP; ++k) {
+        const int p = k * 4 + group;
+        mp[k] = p < parts ? base[p * next + (size_t)16 * D + row] : -INFINITY;
+        M = fmaxf(M, mp[k]);
+    }
+    if ((threadIdx.x & 3) == 0) m_sh[group][row] = M;
+    __syncthreads();
+    M = fmaxf(fmaxf(m_sh[0][row], m_sh[1][row]), fmaxf(m_sh[2][row], m_sh[3][row]));
+#pragma unroll
+    for (int k = 0; k < MAXP; ++k) {
+        const int p = k * 4 + group;
+        if (p >= parts) continue;
+        const float* const sp = base + p * next;
+        // (a part none of whose keys count has a row sum of zero and no reference)
+        const float lp = sp[(size_t)16 * (D + 1) + row], w = lp == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(mp[k] - M);
+        L += w * lp;
+        const f32x4 x = *reinterpret_cast<const f32x4*>(sp + (size_t)row * D + f0), y = *reinterpret_cast<const f32x4*>(sp + (size_t)row * D + f0 + 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            o[e] += w * x[e];
+            o[4 + e] += w * y[e];
         }
-        if (nb > 0) __syncthreads();
-        if ((threadIdx.x & 3) == 0) m_sh[group][row] = M;
-        __syncthreads();
-        M = fmaxf(fmaxf(m_sh[0][row], m_sh[1][row]), fmaxf(m_sh[2][row], m_sh[3][row]));
+    }
 #pragma unroll
-        for (int i = 0; i < MAXP; ++i) {
-            const int p = i * 4 + group;
-            if (p >= parts) continue;
-            const float* const sp = base + (size_t)p * FewSlot<D, NB>::FLOATS;
-            // (a part none of whose keys count has a row sum of zero and no reference)
-            const float lp = sp[(size_t)16 * NB * (D + 1) + col], w = lp == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(mp[i] - M);
-            L += w * lp;
-            const f32x4 x = *reinterpret_cast<const f32x4*>(sp + (size_t)col * D + f0), y = *reinterpret_cast<const f32x4*>(sp + (size_t)col * D + f0 + 4);
+    for (int e = 0; e < 8; ++e) red[group][threadIdx.x & 63][e] = o[e];
+    red[group][threadIdx.x & 63][8] = L;
+    __syncthreads();
+    if (group == 0 && i < rows.rows) {
+        const int t = threadIdx.x;
+        const float inv = 1.0f / ((red[0][t][8] + red[1][t][8]) + (red[2][t][8] + red[3][t][8]));
+        bf16x8 h;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                o[e] += w * x[e];
-                o[4 + e] += w * y[e];
-            }
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) red[group][threadIdx.x & 63][e] = o[e];
-        red[group][threadIdx.x & 63][8] = L;
-        __syncthreads();
-        if (group == 0 && col < rows_here) {
-            const int t = threadIdx.x;
-            const float inv = 1.0f / ((red[0][t][8] + red[1][t][8]) + (red[2][t][8] + red[3][t][8]));
-            bf16x8 h;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) h[e] = f32_to_bf16(((red[0][t][e] + red[1][t][e]) + (red[2][t][e] + red[3][t][e])) * inv);
-            const int tok = LIST ? row_first - rq.row0 : (row_first + col) / a.g, head = kvh * a.g + (LIST ? col : (row_first + col) % a.g);
-            *reinterpret_cast<bf16x8*>(a.out + (size_t)(rq.row0 + tok) * a.ld_out + head * D + f0) = h;
-        }
+        for (int e = 0; e < 8; ++e) h[e] = f32_to_bf16(((red[0][t][e] + red[1][t][e]) + (red[2][t][e] + red[3][t][e])) * inv);
+        *reinterpret_cast<bf16x8*>(a.out + (size_t)(rq.row0 + rows.tok0 + (LIST ? 0 : i / a.g)) * a.ld_out + rows.head(i) * D + f0) = h;
     }
 }
 

@@ -453,7 +453,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_pipelined_kernel(c
                     kt = (global_bytes)tiles.template k_tile<MAY_PAGE>(index);
                     vt = (global_bytes)tiles.template v_tile<MAY_PAGE>(index);
                     block = kb;
-                    return true;
                 };
                 float em, el, eo[D / 64];
                 exact_row<D, false>(qkv + (size_t)(rq.row0 + atok) * ld_qkv + ahead * D, scale_log2e, rq.P + atok, kb0, nkb, tile_at, em, el, eo);

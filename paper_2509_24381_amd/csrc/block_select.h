@@ -102,8 +102,10 @@ __global__ __launch_bounds__(256) void key_bounds_kernel(int n_req, int hkv, int
 //  1. every token's p and n (see the score in the header), int8, into LDS;
 //  2. scores of 16 blocks x 16 tokens per v_mfma_i32_16x16x64_i8 chain (the contraction runs over high and low codes), as keys
 //     that order like the scores, into LDS;
-//  3. a wavefront per token finds the score that the last selected block has, by bisection over the key's bits, and writes the blocks
-//     down in ascending order.
+//  3. a team per token finds the score that the last selected block has, digit by digit of the keys' range (a histogram in LDS per
+//     digit: integers, in any order the same), and writes the blocks down in ascending order.
+// WAVES = 4: four tokens, a wavefront each; bound by the latency of its few dependent steps, so that many are needed at once.  WAVES = 16: one
+// token, for calls of few, whose score step reads the bounds of a long cache (8 KB per KV head and 32 blocks at d = 128).
 struct SelectReq {          // 64 bytes
     uint64_t codes, units;
     int32_t room;
@@ -115,7 +117,7 @@ struct SelectArgs {
     int n_req, hkv, g, halvings;
     const bf16* q;
     long ld_q;
-    int tokens;             // tokens of a workgroup, at most 16
+    int tokens;             // tokens of a workgroup: 1 with WAVES = 16, else at most 4
     int blocks;             // keys there is room for per token in LDS
     int n_blocks, n_first, n_last;
     int* chosen;
@@ -124,16 +126,105 @@ struct SelectArgs {
     uint4* copy_to;
     int copy_chunks, groups;
 };
+constexpr int SELECT_MAX_BLOCKS = 32768;   // 128 KB of keys
 
 RS_DEVICE uint32_t key_of_score(float s) {
     const uint32_t b = __builtin_bit_cast(uint32_t, s + 0.0f);   // (minus zero is zero)
     return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
 
+// What a team shares in LDS.
+template <int WAVES>
+struct SelectTeam {
+    uint32_t hist[256];
+    uint32_t digit, left;            // of a digit's search
+    uint32_t low[WAVES], high[WAVES];
+};
+
+// The take-th largest of key[lo .. hi), 0 < take < hi - lo; *equals: how many of those equal to it belong to the `take`.  TEAM wavefronts.
+template <int TEAM>
+RS_DEVICE uint32_t cut_of_keys(const uint32_t* key, int lo, int hi, int take, SelectTeam<TEAM>& sh, int* equals) {
+    const int lane = threadIdx.x & 63, member = TEAM == 1 ? lane : (int)threadIdx.x, wave = TEAM == 1 ? 0 : (int)threadIdx.x >> 6;
+    const auto meet = [&]() RS_INLINE {
+        if constexpr (TEAM > 1) __syncthreads();
+        else __builtin_amdgcn_wave_barrier();   // (one wavefront's LDS accesses are in order)
+    };
+    uint32_t low = 0xffffffffu, high = 0u;
+    for (int b = lo + member; b < hi; b += 64 * TEAM) {
+        low = min(low, key[b]);
+        high = max(high, key[b]);
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) {
+        low = min(low, (uint32_t)__shfl_xor((int)low, off, WAVE));
+        high = max(high, (uint32_t)__shfl_xor((int)high, off, WAVE));
+    }
+    if constexpr (TEAM > 1) {
+        if (lane == 0) {
+            sh.low[wave] = low;
+            sh.high[wave] = high;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < TEAM; ++w) {
+            low = min(low, sh.low[w]);
+            high = max(high, sh.high[w]);
+        }
+    }
+    uint32_t prefix = 0, left = (uint32_t)take;
+    int top = high == low ? 0 : 32 - __builtin_clz(high - low);   // bits of key - low that are not known yet
+    bool first = true;
+    while (top > 0) {
+        const int shift = max(top - 8, 0);
+        const uint32_t mask = (1u << (top - shift)) - 1u;
+        if (member < 64) *reinterpret_cast<uint4*>(&sh.hist[member * 4]) = make_uint4(0u, 0u, 0u, 0u);
+        meet();
+        for (int b = lo + member; b < hi; b += 64 * TEAM) {
+            const uint32_t x = key[b] - low;
+            if (first || (x >> top) == prefix) atomicAdd(&sh.hist[(x >> shift) & mask], 1u);
+        }
+        meet();
+        if (wave == 0) {   // lane: digits 4 lane .. 4 lane + 3, counted from the largest
+            const uint4 h = *reinterpret_cast<const uint4*>(&sh.hist[lane * 4]);
+            const uint32_t mine = h.x + h.y + h.z + h.w;
+            uint32_t sum = mine;   // of this lane's digits and all larger ones
+#pragma unroll
+            for (int off = 1; off < 64; off <<= 1) {
+                const uint32_t up = (uint32_t)__shfl_down((int)sum, off, WAVE);
+                if (lane + off < 64) sum += up;
+            }
+            const uint32_t above = sum - mine;
+            if (above < left && left <= sum) {   // (one lane)
+                uint32_t rest = left - above, d = 3;
+                const uint32_t count[4] = {h.x, h.y, h.z, h.w};
+#pragma unroll
+                for (int i = 3; i > 0; --i)
+                    if (d == (uint32_t)i && rest > count[i]) {
+                        rest -= count[i];
+                        d = i - 1;
+                    }
+                sh.digit = (uint32_t)lane * 4 + d;
+                sh.left = rest;
+            }
+        }
+        meet();
+        prefix = (prefix << (top - shift)) | sh.digit;
+        left = sh.left;
+        top = shift;
+        first = false;
+        meet();
+    }
+    *equals = (int)left;
+    return low + prefix;
+}
+
 template <int D, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void block_select_kernel(SelectArgs a, InlineTable tab) {
+    constexpr int TEAM = WAVES == 16 ? 16 : 1, TEAMS = WAVES / TEAM, KK = 2 * D / 64;
     extern __shared__ __attribute__((aligned(16))) uint32_t keys[];   // [tokens][blocks]
     __shared__ __attribute__((aligned(16))) int8_t u[16][2 * D];
+    __shared__ __attribute__((aligned(16))) SelectTeam<TEAM> team_sh[TEAMS];
+    __shared__ uint32_t chunk_more[TEAM == 1 ? 1 : SELECT_MAX_BLOCKS / 64], chunk_equal[TEAM == 1 ? 1 : SELECT_MAX_BLOCKS / 64];
     const uint32_t* const table = tab.w;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = blockIdx.y;
     if ((int)blockIdx.x >= a.groups) {
@@ -149,25 +240,42 @@ __global__ __launch_bounds__(64 * WAVES) void block_select_kernel(SelectArgs a, 
     const int s0 = min(a.n_first, b_last), s1 = max(s0, b_last + 1 - a.n_last);
     const bool scored = b_last + 1 > a.n_blocks && s1 > s0;   // (else every token takes all it has, or none but the forced ones)
     if (scored) {
-        constexpr int W = D / 64;   // features of a lane: lane W ..
+        constexpr int W = D / 64;   // features of a lane: W lane ..
         for (int t = wave; t < 16; t += WAVES) {
             int p[W] = {}, n[W] = {};
             if (t < nt) {
                 const bf16* const src = a.q + (size_t)(rq.row0 + t0 + t) * a.ld_q + (size_t)h * a.g * D + lane * W;
+                // eight heads at a time, their loads in flight together
                 float top = 0.0f;
-                for (int i = 0; i < a.g; ++i)
+                for (int i0 = 0; i0 < a.g; i0 += 8) {
+                    float x[8][W];
 #pragma unroll
-                    for (int j = 0; j < W; ++j) top = fmaxf(top, fabsf(limited(bf16_to_f32(src[i * D + j]))));
+                    for (int i = 0; i < 8; ++i)
+#pragma unroll
+                        for (int j = 0; j < W; ++j) x[i][j] = bf16_to_f32(src[min(i0 + i, a.g - 1) * D + j]);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+#pragma unroll
+                        for (int j = 0; j < W; ++j) top = fmaxf(top, fabsf(limited(x[i][j])));
+                }
 #pragma unroll
                 for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, WAVE));
                 const int ex = code_exponent(top);
-                for (int i = 0; i < a.g; ++i)
+                for (int i0 = 0; i0 < a.g; i0 += 8) {
+                    float x[8][W];
 #pragma unroll
-                    for (int j = 0; j < W; ++j) {
-                        const int code = (int)rintf(__builtin_ldexpf(limited(bf16_to_f32(src[i * D + j])), -ex));
-                        p[j] += max(code, 0);
-                        n[j] += max(-code, 0);
-                    }
+                    for (int i = 0; i < 8; ++i)
+#pragma unroll
+                        for (int j = 0; j < W; ++j) x[i][j] = bf16_to_f32(src[min(i0 + i, a.g - 1) * D + j]);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+#pragma unroll
+                        for (int j = 0; j < W; ++j) {
+                            const int code = i0 + i < a.g ? (int)rintf(__builtin_ldexpf(limited(x[i][j]), -ex)) : 0;
+                            p[j] += max(code, 0);
+                            n[j] += max(-code, 0);
+                        }
+                }
             }
             const int half = (1 << a.halvings) >> 1;
 #pragma unroll
@@ -178,71 +286,101 @@ __global__ __launch_bounds__(64 * WAVES) void block_select_kernel(SelectArgs a, 
         }
         __syncthreads();
         const int r = lane & 15, c = lane >> 4;
-        i32x4 uf[2 * D / 64];
+        i32x4 uf[KK];
 #pragma unroll
-        for (int k = 0; k < 2 * D / 64; ++k) uf[k] = *reinterpret_cast<const i32x4*>(&u[r][k * 64 + c * 16]);
+        for (int k = 0; k < KK; ++k) uf[k] = *reinterpret_cast<const i32x4*>(&u[r][k * 64 + c * 16]);
         const int8_t* const codes = reinterpret_cast<const int8_t*>(rq.codes) + (size_t)h * rq.room * 2 * D;
         const float* const units = reinterpret_cast<const float*>(rq.units) + (size_t)h * rq.room;
-        for (int b = s0 + wave * 16; b < s1; b += WAVES * 16) {
-            const int8_t* const src = codes + (size_t)min(b + r, s1 - 1) * 2 * D + c * 16;
-            i32x4 x[2 * D / 64], dot = {0, 0, 0, 0};
+        constexpr int U = 4;   // groups of 16 blocks in flight
+        for (int b = s0 + wave * 16 * U; b < s1; b += WAVES * 16 * U) {
+            i32x4 x[U][KK];
+            float unit[U][4];
 #pragma unroll
-            for (int k = 0; k < 2 * D / 64; ++k) x[k] = *reinterpret_cast<const i32x4*>(src + k * 64);
-            float unit[4];
+            for (int v = 0; v < U; ++v) {
+                const int8_t* const src = codes + (size_t)min(b + v * 16 + r, s1 - 1) * 2 * D + c * 16;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) unit[e] = units[min(b + c * 4 + e, s1 - 1)];
+                for (int k = 0; k < KK; ++k) x[v][k] = *reinterpret_cast<const i32x4*>(src + k * 64);
 #pragma unroll
-            for (int k = 0; k < 2 * D / 64; ++k) dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[k], uf[k], dot, 0, 0, 0);
-            if (r < nt) {
+                for (int e = 0; e < 4; ++e) unit[v][e] = units[min(b + v * 16 + c * 4 + e, s1 - 1)];
+            }
 #pragma unroll
-                for (int e = 0; e < 4; ++e)   // block b + 4 c + e, token r
-                    if (b + c * 4 + e < s1) keys[r * a.blocks + b + c * 4 + e - s0] = key_of_score((float)dot[e] * unit[e]);
+            for (int v = 0; v < U; ++v) {
+                i32x4 dot = {0, 0, 0, 0};
+#pragma unroll
+                for (int k = 0; k < KK; ++k) dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[v][k], uf[k], dot, 0, 0, 0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {   // block b + 16 v + 4 c + e, token r
+                    const int block = b + v * 16 + c * 4 + e;
+                    if (r < nt && block < s1) keys[r * a.blocks + block - s0] = key_of_score((float)dot[e] * unit[v][e]);
+                }
             }
         }
         __syncthreads();
     }
-    for (int t = wave; t < nt; t += WAVES) {
+    const unsigned long long below = lane == 0 ? 0ull : ~0ull >> (64 - lane);   // the lanes before this one
+    for (int t = TEAM == 1 ? wave : 0; t < nt; t += TEAMS) {
         const int own = (rq.P + t0 + t) / 64;
         const int lo = min(a.n_first, own + 1), hi = max(lo, own + 1 - a.n_last);   // blocks lo .. hi - 1 compete
         const int take = min(max(a.n_blocks - (own + 1 - (hi - lo)), 0), hi - lo);
         const uint32_t* const key = keys + t * a.blocks - s0;
-        // the take-th largest key: `cut`; of the blocks that have it, the first `equals`
-        uint32_t cut = 0;
+        uint32_t cut = 0;   // the take-th largest key; of the blocks that have it, the first `equals`
         int equals = 0;
-        if (take > 0 && take < hi - lo) {
-            int above = 0;   // keys above the range that is left
-            uint32_t bit = 0x80000000u;
-            for (; bit; bit >>= 1) {
-                const uint32_t mid = cut | bit;
-                int count = 0;
-                for (int b = lo + lane; b < hi; b += 64) count += key[b] >= mid;
-#pragma unroll
-                for (int off = 32; off > 0; off >>= 1) count += __shfl_xor(count, off, WAVE);
-                if (count >= take) cut = mid;
-                else above = count;
-            }
-            equals = take - above;
-        }
+        const bool some = take > 0 && take < hi - lo;
+        if (some) cut = cut_of_keys<TEAM>(key, lo, hi, take, team_sh[TEAM == 1 ? wave : 0], &equals);
         int* const out = a.chosen + ((size_t)(rq.row0 + t0 + t) * a.hkv + h) * a.n_blocks;
-        int done = 0;
-        for (int b0 = 0; b0 <= own && done < a.n_blocks; b0 += 64) {
-            const int b = b0 + lane;
-            bool sel = b < lo || (b >= hi && b <= own);
-            if (b >= lo && b < hi) sel = take == hi - lo;
-            bool eq = false;
-            if (take > 0 && take < hi - lo && b >= lo && b < hi) {
-                sel = key[b] > cut;
-                eq = key[b] == cut;
+        // is block b taken for sure; does it have the cut's key
+        const auto taken = [&](int b, bool& eq) RS_INLINE {
+            const bool competes = b >= lo && b < hi;
+            const uint32_t k = some && competes ? key[b] : 0u;
+            eq = some && competes && k == cut;
+            return competes ? (some ? k > cut : take > 0) : b <= own;
+        };
+        const int chunks = own / 64 + 1;   // of 64 blocks
+        if constexpr (TEAM == 1) {
+            int done = 0;
+            for (int ch = 0; ch < chunks && done < a.n_blocks; ++ch) {
+                bool eq;
+                bool sel = taken(ch * 64 + lane, eq);
+                const unsigned long long eqs = __builtin_amdgcn_ballot_w64(eq);
+                if (eq) sel = __popcll(eqs & below) < equals;
+                equals -= min(equals, (int)__popcll(eqs));
+                const unsigned long long sels = __builtin_amdgcn_ballot_w64(sel);
+                const int at = done + (int)__popcll(sels & below);
+                if (sel && at < a.n_blocks) out[at] = ch * 64 + lane;
+                done += (int)__popcll(sels);
             }
-            const unsigned long long below = lane == 0 ? 0ull : ~0ull >> (64 - lane);
-            const unsigned long long eqs = __builtin_amdgcn_ballot_w64(eq);
-            if (eq) sel = __popcll(eqs & below) < equals;
-            equals -= min(equals, (int)__popcll(eqs));
-            const unsigned long long sels = __builtin_amdgcn_ballot_w64(sel);
-            const int at = done + (int)__popcll(sels & below);
-            if (sel && at < a.n_blocks) out[at] = b;
-            done += (int)__popcll(sels);
+            for (int i = min(done, a.n_blocks) + lane; i < a.n_blocks; i += 64) out[i] = -1;
+        } else {
+            for (int ch = wave; ch < chunks; ch += TEAM) {
+                bool eq;
+                const bool sel = taken(ch * 64 + lane, eq);
+                const uint32_t more = (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(sel)), equal = (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(eq));
+                if (lane == 0) {
+                    chunk_more[ch] = more;
+                    chunk_equal[ch] = equal;
+                }
+            }
+            __syncthreads();
+            for (int ch = wave; ch < chunks; ch += TEAM) {
+                int more = 0, equal = 0;   // in the chunks before this one
+                for (int i = lane; i < ch; i += 64) {
+                    more += (int)chunk_more[i];
+                    equal += (int)chunk_equal[i];
+                }
+#pragma unroll
+                for (int off = 32; off > 0; off >>= 1) {
+                    more += __shfl_xor(more, off, WAVE);
+                    equal += __shfl_xor(equal, off, WAVE);
+                }
+                bool eq;
+                bool sel = taken(ch * 64 + lane, eq);
+                if (eq) sel = equal + (int)__popcll(__builtin_amdgcn_ballot_w64(eq) & below) < equals;
+                const unsigned long long sels = __builtin_amdgcn_ballot_w64(sel);
+                const int at = more + min(equal, equals) + (int)__popcll(sels & below);
+                if (sel && at < a.n_blocks) out[at] = ch * 64 + lane;
+            }
+            const int all = min(a.n_blocks, own + 1);
+            for (int i = all + (int)threadIdx.x; i < a.n_blocks; i += 64 * TEAM) out[i] = -1;
         }
-        for (int i = min(done, a.n_blocks) + lane; i < a.n_blocks; i += 64) out[i] = -1;
     }
 }

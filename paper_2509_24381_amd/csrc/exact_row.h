@@ -23,7 +23,7 @@ RS_DEVICE void exact_row(const bf16* q, float sc, int qpos, int i0, int i1, Tile
     for (int i = i0; i < i1; ++i) {
         global_bytes kt, vt;
         int block;
-        if (!tile_at(i, kt, vt, block)) continue;
+        tile_at(i, kt, vt, block);
         const int live = min(64, qpos + 1 - block * 64);   // keys that the row sees
         if (live <= 0) continue;
         float s = 0.0f;

@@ -28,8 +28,9 @@ struct rs_rotary {
 namespace {
 
 constexpr int FEW_ROWS = 64;       // stacked rows of a request up to which it goes to attend_few_kernel
+constexpr int FEW_PLACES = 2;      // workgroups of attend_few_kernel that a compute unit holds
 constexpr size_t SLOT_ROWS = 65536;   // rows there is room for in the slots of split key ranges
-constexpr size_t SELECT_LDS = (size_t)128 << 10;
+constexpr size_t SELECT_LDS = (size_t)SELECT_MAX_BLOCKS * 4;
 
 // ---- checks that all calls share; *rows_out: the sum of lens (null lens: none)
 rs_status check_call(const rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, bool need_lens, int R, long* rows_out) {
@@ -105,14 +106,6 @@ void for_kind(const rs_ctx* c, bool fp8, F&& f) {
         else f(std::integral_constant<int, 64>{}, std::false_type{});
     }
 }
-template <class F>
-void for_row_blocks(int rows, F&& f) {   // blocks of 16 rows
-    if (rows <= 16) f(std::integral_constant<int, 1>{});
-    else if (rows <= 32) f(std::integral_constant<int, 2>{});
-    else f(std::integral_constant<int, 4>{});
-}
-int row_blocks(int rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
-
 // ---------------------------------------------------------------- bounds
 rs_status check_bounds(const rs_kv* kv, int layer, int i) {
     if (!kv->bound_codes) return fail(RS_ESTATE, "kvs[%d] has no memory for bounds (rs_kv_attach_bounds)", i);
@@ -209,7 +202,8 @@ size_t expansion_bytes(const rs_ctx* c, long tokens) { return (size_t)2 * align_
 // once, the share of each place plus half a part, and two tiles for joining.
 struct FewRequest {
     int kv, row0, T;       // index into kvs, first row, rows
-    int units, tiles;      // row blocks times KV heads, tiles
+    int units, tiles;      // items per part, tiles
+    int row_blocks;        // of 16 rows
     int parts;
 };
 void plan_few(std::vector<FewRequest>& reqs, int places, size_t slots) {
@@ -227,7 +221,7 @@ void plan_few(std::vector<FewRequest>& reqs, int places, size_t slots) {
         for (const FewRequest& r : reqs) {
             const int p = std::min((r.tiles + len - 1) / len, FEW_MAX_PARTS);
             items += (long)r.units * p;
-            if (p > 1) split += (long)r.units * p;
+            if (p > 1) split += (long)r.units * p * r.row_blocks;
             most = std::max(most, (r.tiles + p - 1) / p);
         }
         const double cost = (items <= places ? most : std::max<double>(most, (double)total / places + 0.5 * most)) + (split ? 2.0 : 0.0);
@@ -268,9 +262,9 @@ FewTable write_few_table(const rs_ctx* ctx, int layer, rs_kv* const* kvs, const 
         w[j] = list ? (uint32_t)r.row0 : t.items;
         w[table_units_at(n) + j] = t.units;
         t.items += (uint32_t)(r.units * r.parts);
-        t.units += (uint32_t)r.units;
+        t.units += (uint32_t)(r.units * r.row_blocks);
         if (r.parts > 1) {
-            slot += r.units * r.parts;
+            slot += r.units * r.parts * r.row_blocks;
             t.any_split = true;
         }
     }
@@ -283,21 +277,19 @@ size_t few_table_words(const rs_ctx*, rs_kv* const* kvs, const std::vector<FewRe
 }
 
 template <bool LIST>
-rs_status launch_few(const rs_ctx* ctx, bool fp8, int rows, const FewArgs& a, uint32_t items, uint32_t units, bool split, const InlineTable* tab, hipStream_t st) {
+rs_status launch_few(const rs_ctx* ctx, bool fp8, const FewArgs& a, uint32_t items, uint32_t units, bool split, const InlineTable* tab, hipStream_t st) {
     for_kind(ctx, fp8, [&](auto d, auto f8) {
-        for_row_blocks(rows, [&](auto nb) {
-            constexpr int D = decltype(d)::value, NB = decltype(nb)::value;
-            constexpr bool FP8 = decltype(f8)::value;
-            if constexpr (!LIST) {
-                if (tab) {
-                    hipLaunchKernelGGL((attend_few_kernel<D, FP8, NB, false, true>), dim3(items), dim3(64 * FEW_WAVES), 0, st, a, *tab);
-                    if (split) hipLaunchKernelGGL((few_merge_kernel<D, NB, false, true>), dim3(units, D / 32), dim3(256), 0, st, a, *tab);
-                    return;
-                }
+        constexpr int D = decltype(d)::value;
+        constexpr bool FP8 = decltype(f8)::value;
+        if constexpr (!LIST) {
+            if (tab) {
+                hipLaunchKernelGGL((attend_few_kernel<D, FP8, false, true>), dim3(items), dim3(64 * FEW_WAVES), 0, st, a, *tab);
+                if (split) hipLaunchKernelGGL((few_merge_kernel<D, false, true>), dim3(units, D / 32), dim3(256), 0, st, a, *tab);
+                return;
             }
-            hipLaunchKernelGGL((attend_few_kernel<D, FP8, NB, LIST, false>), dim3(items), dim3(64 * FEW_WAVES), 0, st, a, NoTable{});
-            if (split) hipLaunchKernelGGL((few_merge_kernel<D, NB, LIST, false>), dim3(units, D / 32), dim3(256), 0, st, a, NoTable{});
-        });
+        }
+        hipLaunchKernelGGL((attend_few_kernel<D, FP8, LIST, false>), dim3(items), dim3(64 * FEW_WAVES), 0, st, a, NoTable{});
+        if (split) hipLaunchKernelGGL((few_merge_kernel<D, LIST, false>), dim3(units, D / 32), dim3(256), 0, st, a, NoTable{});
     });
     RS_HIP(hipGetLastError());
     return RS_OK;
@@ -588,13 +580,11 @@ rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, 
 
     // ---- requests of few rows
     std::vector<FewRequest> few;
-    int row = 0, most_rows = 0;
+    int row = 0;
     for (int i = 0; i < R; ++i) {
-        const int stacked = (int)std::min<long>((long)lens[i] * ctx->group, FEW_ROWS + 1);
-        if (lens[i] > 0 && stacked <= FEW_ROWS) {
-            few.push_back(FewRequest{i, row, lens[i], 0, (kvs[i]->len[layer] + 63) / 64, 1});
-            most_rows = std::max(most_rows, stacked);
-        }
+        const long stacked = (long)lens[i] * ctx->group;
+        if (lens[i] > 0 && stacked <= FEW_ROWS)
+            few.push_back(FewRequest{i, row, lens[i], f.n_kv_heads, (kvs[i]->len[layer] + 63) / 64, few_row_blocks((int)stacked), 1});
         row += lens[i];
     }
     FewArgs a{};
@@ -603,9 +593,7 @@ rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, 
     bool inline_table = false;
     size_t few_words = 0;
     if (!few.empty()) {
-        const int nb = row_blocks(most_rows);
-        for (FewRequest& r : few) r.units = f.n_kv_heads;   // (one block of rows: at most 16 nb)
-        plan_few(few, ctx->n_cu * (nb == 1 ? 2 : 1), SLOT_ROWS / (16 * nb));
+        plan_few(few, FEW_PLACES * ctx->n_cu, SLOT_ROWS / 16);
         a.n_req = (int)few.size();
         a.hkv = f.n_kv_heads; a.g = ctx->group;
         a.q = (const bf16*)q; a.ld_q = ld_q; a.out = (bf16*)out; a.ld_out = ld_out;
@@ -685,7 +673,7 @@ rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, 
         if ((s = ring_commit(ctx, st)) != RS_OK) return s;
     }
     if (!few.empty() &&
-        (s = launch_few<false>(ctx, fp8, most_rows, a, ft.items, ft.units, ft.any_split, inline_table ? &tab : nullptr, st)) != RS_OK)
+        (s = launch_few<false>(ctx, fp8, a, ft.items, ft.units, ft.any_split, inline_table ? &tab : nullptr, st)) != RS_OK)
         return s;
     if (!chunks) return RS_OK;
     const ReqDesc* const d_reqs = reinterpret_cast<const ReqDesc*>(ws + at_reqs);
@@ -757,7 +745,7 @@ rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int*
     const rs_layer_cfg& f = ctx->cfg;
     int longest = 0;
     for (int i = 0; i < R; ++i) longest = std::max(longest, lens[i] > 0 ? kvs[i]->len[layer] / 64 + 1 : 0);
-    if ((size_t)longest * 4 > SELECT_LDS) return fail(RS_ECAPACITY, "a cache of %d blocks is longer than the selection can hold (%zu)", longest, SELECT_LDS / 4);
+    if (longest > SELECT_MAX_BLOCKS) return fail(RS_ECAPACITY, "a cache of %d blocks is longer than the selection can hold (%d)", longest, SELECT_MAX_BLOCKS);
     if (chosen && !aligned(chosen, 4)) return fail(RS_EINVAL, "chosen must be 4-byte aligned");
     const AttendLayout L = attend_layout(f, (int)rows, R, n_blocks);
     if ((s = check_workspace(workspace, workspace_bytes, L.total)) != RS_OK) return s;
@@ -789,14 +777,14 @@ rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int*
     std::vector<FewRequest> reqs;
     int row = 0;
     for (int i = 0; i < R; ++i) {
-        if (lens[i] > 0) reqs.push_back(FewRequest{i, row, lens[i], lens[i] * f.n_kv_heads, (kvs[i]->len[layer] + 63) / 64, 1});
+        if (lens[i] > 0) reqs.push_back(FewRequest{i, row, lens[i], lens[i] * f.n_kv_heads, (kvs[i]->len[layer] + 63) / 64, few_row_blocks(ctx->group), 1});
         row += lens[i];
     }
-    const int nb = row_blocks(ctx->group), units = (int)rows * f.n_kv_heads;
+    const int rbn = few_row_blocks(ctx->group), units = (int)rows * f.n_kv_heads;
     int parts = 1;
-    const int places = ctx->n_cu * (nb == 1 ? 2 : 1);
+    const int places = FEW_PLACES * ctx->n_cu;
     if (units < places) parts = std::min((std::min(n_blocks, longest) + FEW_WAVES - 1) / FEW_WAVES, (places + units - 1) / units);
-    while (parts > 1 && (size_t)units * parts > SLOT_ROWS / (16 * nb)) --parts;
+    while (parts > 1 && (size_t)units * parts * rbn > SLOT_ROWS / 16) --parts;
     parts = std::max(1, std::min(parts, FEW_MAX_PARTS));
     int slot = 0;
     if ((s = ring_acquire(ctx, st, &slot)) != RS_OK) return s;
@@ -862,7 +850,7 @@ rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int*
     a.chosen = list;
     a.n_blocks = n_blocks;
     a.list_parts = parts;
-    return launch_few<true>(ctx, fp8, ctx->group, a, (uint32_t)(units * parts), (uint32_t)units, parts > 1, nullptr, st);
+    return launch_few<true>(ctx, fp8, a, (uint32_t)(units * parts), (uint32_t)(units * rbn), parts > 1, nullptr, st);
 }
 
 }  // extern "C"
