@@ -5,8 +5,8 @@
 //
 // Bound by the bytes of the keys and values: a tile of 64 keys is 32 KB (d = 128, bfloat16), and the rows that share it - the g
 // query heads of a KV head, times the tokens - give it 16 MFMAs of 16 clocks per 16 rows and product.  So wavefronts share no tiles: each
-// streams its own through its own LDS, by DMA, without barriers, in units of 8 KB of keys and 8 KB of values: the next unit's keys
-// are under way as soon as this one's are in registers, its values likewise.  (Loads straight into the MFMA operand layout, where
+// streams its own through its own LDS, by DMA, without barriers, in units of 8 KB - a tile's keys, then its values - and two places: the unit
+// after the next is under way as soon as this one is in registers.  (Loads straight into the MFMA operand layout, where
 // neighbouring lanes are different keys, need no LDS, but the address unit then takes 64 clocks for a load of a KB instead of 16: a
 // compute unit gets 16 bytes per clock, whatever the cache they come from.)
 //
@@ -114,19 +114,19 @@ struct FewRows {
     __device__ __forceinline__ int head(int i) const { return kvh * g + (LIST ? i : i % g); }
 };
 
-// A wavefront's unit of work: KEYS keys of a tile, their K rows and V^T columns BYTES each in LDS.  16-byte chunks sit at places of their row
-// that make the 8 lanes of a read, which are 8 keys or features of one chunk, meet different banks; a load instruction fills 1 KB of LDS
-// linearly by lane, each lane fetching the chunk that belongs in its place.
+// How a wavefront streams a tile: its keys, then its values (V^T), in PER units each of BYTES contiguous bytes.  16-byte chunks sit at places
+// of their row that make the 8 lanes of a read, which are 8 keys or features of one chunk, meet different banks; a load instruction
+// fills 1 KB of LDS linearly by lane, each lane fetching the chunk that belongs in its place.
 template <int D, bool FP8>
 struct FewUnit {
     static constexpr int EL = FP8 ? 1 : 2;
-    static constexpr int TILE = 64 * D * EL;                          // bytes of a tile
-    static constexpr int PER_TILE = TILE > 8192 ? TILE / 8192 : 1;
-    static constexpr int KEYS = 64 / PER_TILE, BYTES = TILE / PER_TILE, LOADS = BYTES / 1024;
-    static constexpr int K_ROW = D * EL, K_CHUNKS = K_ROW / 16;       // a key's bytes, chunks
-    static constexpr int K_READS = K_CHUNKS / 4;                      // 16-byte reads of a lane per 16 keys
-    static constexpr int V_TILE_ROW = 64 * EL, V_ROW = KEYS * EL;     // a feature's bytes in the tile, in the unit
-    static constexpr int V_CHUNKS = V_ROW / 64;                       // 16-byte reads of a lane per 16 features
+    static constexpr int TILE = 64 * D * EL;                    // bytes of a tile's keys, or values
+    static constexpr int PER = TILE > 8192 ? TILE / 8192 : 1;
+    static constexpr int BYTES = TILE / PER, LOADS = BYTES / 1024;
+    static constexpr int K_ROW = D * EL, K_CHUNKS = K_ROW / 16;   // a key's bytes, chunks
+    static constexpr int K_READS = K_CHUNKS / 4;                // 16-byte reads of a lane per 16 keys
+    static constexpr int V_ROW = 64 * EL;                       // a feature's bytes
+    static constexpr int V_READS = V_ROW / 64;                  // 16-byte reads of a lane per 16 features
     // Key of MFMA row i of sub-tile t: the scores a lane ends up with - rows 4 c .. 4 c + 3 of every sub-tile - are the keys it multiplies
     // with values, consecutive ones: 8 of every 32, or with 8-bit values, which come 16 to a chunk, 16 of 64.
     RS_UNIT static int key_of(int t, int i) {
@@ -139,26 +139,19 @@ struct FewUnit {
     RS_UNIT static int v_swizzle(int feature) { return V_ROW == 128 ? feature & 7 : (feature >> 1) & 3; }
     RS_UNIT static uint32_t k_place(int key, int chunk) { return (uint32_t)(key * K_ROW + (chunk ^ k_swizzle(key)) * 16); }
     RS_UNIT static uint32_t v_place(int feature, int chunk) { return (uint32_t)(feature * V_ROW + (chunk ^ v_swizzle(feature)) * 16); }
-    // bytes from a lane's chunks of sub-tile 0 to those of sub-tile t (the swizzle is the MFMA row's: the same)
+    // bytes from a lane's chunks of sub-tile 0 to those of sub-tile t (the swizzle is the MFMA row's: the same); a unit has 4 / PER sub-tiles
     RS_UNIT static constexpr int k_step(int t) { return (FP8 ? t * 4 : (t >> 1) * 32 + (t & 1) * 4) * K_ROW; }
-    // where in the tile the chunk that belongs at place p of the unit is
-    RS_UNIT static uint32_t k_source(int p) {
-        const int key = p / K_CHUNKS;
-        return (uint32_t)(key * K_ROW + (p % K_CHUNKS ^ k_swizzle(key)) * 16);
-    }
-    RS_UNIT static uint32_t v_source(int p) {
-        const int f = p / (V_ROW / 16);
-        return (uint32_t)(f * V_TILE_ROW + (p % (V_ROW / 16) ^ v_swizzle(f)) * 16);
-    }
-    // load instructions after which the keys' sources repeat, as many keys further on
+    // where in the unit the chunk that belongs at place p (16 bytes each) is
+    RS_UNIT static uint32_t k_source(int p) { return k_place(p / K_CHUNKS, p % K_CHUNKS); }
+    RS_UNIT static uint32_t v_source(int p) { return v_place(p / (V_ROW / 16), p % (V_ROW / 16)); }
+    // load instructions after which the keys' sources repeat, as many keys further on (values': every one, a KB is 8 or 16 features)
     static constexpr int K_PATTERNS = (FP8 ? 64 : 32) * K_ROW / 1024 < LOADS ? (FP8 ? 64 : 32) * K_ROW / 1024 : LOADS;
-    // (values: every one; a KB is 8 or 16 features)
 };
 
 template <int D, bool FP8, bool LIST, bool INLINE>
 __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a, std::conditional_t<INLINE, InlineTable, NoTable> tab) {
     typedef FewUnit<D, FP8> U;
-    constexpr int KS = D / 32, DT = D / 16, NT = U::KEYS / 16;
+    constexpr int KS = D / 32, DT = D / 16, NT = 4 / U::PER, DTU = DT / U::PER;   // sub-tiles of a K unit, feature blocks of a V unit
     __shared__ __attribute__((aligned(16))) char lds[FEW_WAVES * 2 * U::BYTES];   // each wavefront's keys and values, in the end its sums
     __shared__ float m_sh[FEW_WAVES][16], l_sh[FEW_WAVES][16];
     const uint32_t* const table = table_of<INLINE>(tab, a.table);
@@ -239,34 +232,23 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
         place = rq.pages == CONTIGUOUS ? number : (int)table[rq.pages + number];
     };
     typedef __attribute__((address_space(3))) void* lds_ptr;
-    char* const k_mine = lds + wave * 2 * U::BYTES;
-    char* const v_mine = k_mine + U::BYTES;
+    char* const mine = lds + wave * 2 * U::BYTES;
     const uint64_t k_head = rq.k + (uint64_t)rows.kvh * rq.head_bytes, v_head = rq.v + (uint64_t)rows.kvh * rq.head_bytes;
     uint32_t k_src[8];   // where a lane's 16 bytes of a load instruction come from (U::K_PATTERNS of them; values: one)
 #pragma unroll
     for (int i = 0; i < U::K_PATTERNS; ++i) k_src[i] = U::k_source(i * 64 + lane);
     const uint32_t v_src = U::v_source(lane);
-    const auto tile_of = [&](uint64_t head, int j) RS_INLINE {
-        return (void*)(head + (uint64_t)(uint32_t)__builtin_amdgcn_readlane(place, j & 63) * rq.block_bytes);
-    };
-    const auto fetch_k = [&](int u) RS_INLINE {
-        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(tile_of(k_head, u / U::PER_TILE), 0, U::TILE, 0x00020000);
-        const int soff = u % U::PER_TILE * U::BYTES;   // (keys are rows: a unit is contiguous)
+    // unit h of tile j: 0 .. PER - 1 its keys, then its values; unit h goes to place h & 1
+    const auto fetch = [&](int j, int h) RS_INLINE {
+        const bool keys = h < U::PER;
+        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+            (void*)((keys ? k_head : v_head) + (uint64_t)(uint32_t)__builtin_amdgcn_readlane(place, j & 63) * rq.block_bytes), 0, U::TILE, 0x00020000);
+        char* const to = mine + (h & 1) * U::BYTES;
 #pragma unroll
         for (int i = 0; i < U::LOADS; ++i) {
-            const uint32_t from = k_src[i % U::K_PATTERNS];   // (named: template-dependent arguments of the builtin break the host-side stub)
-            const int further = soff + i / U::K_PATTERNS * U::K_PATTERNS * 1024;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)(uintptr_t)(uint32_t)(uintptr_t)(k_mine + i * 1024), 16, from, further, 0, 0);
-        }
-    };
-    const auto fetch_v = [&](int u) RS_INLINE {
-        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(tile_of(v_head, u / U::PER_TILE), 0, U::TILE, 0x00020000);
-        const int soff = u % U::PER_TILE * U::V_ROW;   // (of every feature's row of 64 keys, the unit's part)
-#pragma unroll
-        for (int i = 0; i < U::LOADS; ++i) {
-            const uint32_t from = v_src;   // (named: template-dependent arguments of the builtin break the host-side stub)
-            const int further = soff + i * 1024 / U::V_ROW * U::V_TILE_ROW;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)(uintptr_t)(uint32_t)(uintptr_t)(v_mine + i * 1024), 16, from, further, 0, 0);
+            const uint32_t from = keys ? k_src[i % U::K_PATTERNS] : v_src;   // (named: template-dependent arguments of the builtin break the host-side stub)
+            const int further = h % U::PER * U::BYTES + (keys ? i / U::K_PATTERNS * U::K_PATTERNS : i) * 1024;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)(uintptr_t)(uint32_t)(uintptr_t)(to + i * 1024), 16, from, further, 0, 0);
         }
     };
     // (the compiler does not see LDS written by DMA, nor may it move a refill above the reads of what it overwrites)
@@ -284,53 +266,64 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
 #pragma unroll
     for (int i = 0; i < U::K_READS; ++i) k_at[i] = U::k_place(U::key_of(0, r), i * 4 + c);
 #pragma unroll
-    for (int i = 0; i < U::V_CHUNKS; ++i) v_at[i] = U::v_place(r, i * 4 + c);
+    for (int i = 0; i < U::V_READS; ++i) v_at[i] = U::v_place(r, i * 4 + c);
 
-    const int units = tiles * U::PER_TILE;
-    if (units > 0) {
+    if (tiles > 0) {
         look_up(0);
-        fetch_k(0);
-        fetch_v(0);
+        fetch(0, 0);
+        fetch(0, 1);
     }
-    int block = 0;
-    for (int u = 0; u < units; ++u) {
-        if (u % U::PER_TILE == 0) block = __builtin_amdgcn_readlane(number, u / U::PER_TILE & 63);
-        const int key0 = block * 64 + u % U::PER_TILE * U::KEYS;
-        const bool more = u + 1 < units;
-        // (places are needed up to one unit ahead)
-        if (more && (u + 1) % (64 * U::PER_TILE) == 0) look_up((u + 1) / U::PER_TILE);
-        wait_loads(true);
-        uint4 kf[NT * U::K_READS];
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int i = 0; i < U::K_READS; ++i)
-                kf[t * U::K_READS + i] = *reinterpret_cast<const uint4*>(k_mine + k_at[i] + U::k_step(t));
-        reads_done();
-        if (more) fetch_k(u + 1);
-        f32x4 s[NT];
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int kk = 0; kk < KS; ++kk) {
-                bf16x8 kfrag;
-                if constexpr (FP8) {
-                    const uint4 w = kf[t * U::K_READS + (kk >> 1)];
-                    kfrag = (kk & 1) ? bf16x8_of_codes(w.z, w.w) : bf16x8_of_codes(w.x, w.y);
-                } else {
-                    kfrag = as_bf16x8(kf[t * U::K_READS + kk]);
-                }
-                s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kfrag, qf[kk], kk == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : s[t], 0, 0, 0);
+    int block = __builtin_amdgcn_readlane(number, 0);
+    for (int j = 0; j < tiles; ++j) {
+        const int key0 = block * 64;
+        const bool more = j + 1 < tiles;
+        f32x4 s[4];
+        // (the unit after the next: of this tile, or, places looked up in time, of the next one)
+        const auto refill = [&](auto hc) RS_INLINE {
+            constexpr int h = decltype(hc)::value, n = h + 2;
+            if constexpr (n < 2 * U::PER) {
+                fetch(j, n);
+            } else {
+                if constexpr (n == 2 * U::PER)
+                    if (more && ((j + 1) & 63) == 0) look_up(j + 1);
+                if (more) fetch(j + 1, n - 2 * U::PER);
             }
-        if (key0 + U::KEYS - 1 > seen_by_all) {
+        };
+        static_for<0, U::PER>([&](auto hc) RS_INLINE {
+            constexpr int h = decltype(hc)::value;
+            wait_loads(true);
+            uint4 kf[8];
 #pragma unroll
             for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < U::K_READS; ++i)
+                    kf[t * U::K_READS + i] = *reinterpret_cast<const uint4*>(mine + (h & 1) * U::BYTES + k_at[i] + U::k_step(t));
+            reads_done();
+            refill(hc);
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int kk = 0; kk < KS; ++kk) {
+                    bf16x8 kfrag;
+                    if constexpr (FP8) {
+                        const uint4 w = kf[t * U::K_READS + (kk >> 1)];
+                        kfrag = (kk & 1) ? bf16x8_of_codes(w.z, w.w) : bf16x8_of_codes(w.x, w.y);
+                    } else {
+                        kfrag = as_bf16x8(kf[t * U::K_READS + kk]);
+                    }
+                    f32x4& to = s[h * NT + t];
+                    to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kfrag, qf[kk], kk == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : to, 0, 0, 0);
+                }
+        });
+        if (key0 + 63 > seen_by_all) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[t][e] = key0 + U::key_of(t, c * 4 + e) <= qpos ? s[t][e] : -INFINITY;
         }
         float mx = s[0][0];
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[t][e]);
         mx = fmaxf(mx, __shfl_xor(mx, 16, WAVE));
@@ -347,33 +340,38 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
                 for (int e = 0; e < 4; ++e) acc[dt][e] *= alpha;
         }
         const float ref = m == -INFINITY ? 0.0f : m;
-        bf16x8 pf[NT / 2];
+        bf16x8 pf[2];
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e], sc, -ref));
                 l += p;
                 pf[t >> 1][(t & 1) * 4 + e] = f32_to_bf16(p);
             }
-        wait_loads(more);
-        uint4 vf[DT * U::V_CHUNKS];
+        static_for<0, U::PER>([&](auto hc) RS_INLINE {
+            constexpr int h = decltype(hc)::value;
+            wait_loads(h + 1 < U::PER || more);
+            uint4 vf[8];
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
+            for (int dt = 0; dt < DTU; ++dt)
 #pragma unroll
-            for (int i = 0; i < U::V_CHUNKS; ++i)
-                vf[dt * U::V_CHUNKS + i] = *reinterpret_cast<const uint4*>(v_mine + v_at[i] + dt * 16 * U::V_ROW);
-        reads_done();
-        if (more) fetch_v(u + 1);
+                for (int i = 0; i < U::V_READS; ++i)
+                    vf[dt * U::V_READS + i] = *reinterpret_cast<const uint4*>(mine + ((U::PER + h) & 1) * U::BYTES + v_at[i] + dt * 16 * U::V_ROW);
+            reads_done();
+            refill(std::integral_constant<int, U::PER + h>{});
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
+            for (int dt = 0; dt < DTU; ++dt)
 #pragma unroll
-            for (int s2 = 0; s2 < NT / 2; ++s2) {
-                bf16x8 vfrag;
-                if constexpr (FP8) vfrag = s2 ? bf16x8_of_codes(vf[dt].z, vf[dt].w) : bf16x8_of_codes(vf[dt].x, vf[dt].y);
-                else vfrag = as_bf16x8(vf[dt * U::V_CHUNKS + s2]);
-                acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vfrag, pf[s2], acc[dt], 0, 0, 0);
-            }
+                for (int s2 = 0; s2 < 2; ++s2) {
+                    bf16x8 vfrag;
+                    if constexpr (FP8) vfrag = s2 ? bf16x8_of_codes(vf[dt].z, vf[dt].w) : bf16x8_of_codes(vf[dt].x, vf[dt].y);
+                    else vfrag = as_bf16x8(vf[dt * U::V_READS + s2]);
+                    f32x4& to = acc[h * DTU + dt];
+                    to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vfrag, pf[s2], to, 0, 0, 0);
+                }
+        });
+        block = __builtin_amdgcn_readlane(number, (j + 1) & 63);
     }
 
     static_assert(16 * (D + 4) * 4 <= 2 * U::BYTES, "a wavefront's sums fit where its keys and values were");

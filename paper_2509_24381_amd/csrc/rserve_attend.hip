@@ -620,8 +620,9 @@ rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, 
     std::vector<AttnRequest> att;
     AttnPlan plan;
     int n_xblocks = 0;
-    const size_t at_reqs = L.few, at_items = at_reqs + L.reqs, at_pages = at_items + L.items, at_mitems = at_pages + L.pagetab, at_fp8 = at_mitems + L.mitems;
+    size_t at_reqs = 0, at_items = 0, at_mitems = 0, at_fp8 = 0;   // (packed: what is staged crosses the host link)
     if (chunks) {
+        const size_t at_pages = staged_bytes;
         const int* const d_pagetab = reinterpret_cast<const int*>(ws + at_pages);
         size_t expand_at = L.total;
         row = 0;
@@ -655,15 +656,17 @@ rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, 
             att.push_back(AttnRequest{lens[i], d.P});
         }
         plan = plan_attention(AttnPlanSettings{ctx->n_cu, ctx->attn_split, ctx->attn_plain_order}, att, ctx->group, f.n_kv_heads);
-        if (sizeof(ReqDesc) * reqs.size() > L.reqs || sizeof(AttnItem) * plan.items.size() > L.items || sizeof(int) * pagetab.size() > L.pagetab ||
-            sizeof(AttnMergeItem) * plan.merges.size() > L.mitems || sizeof(Fp8CacheDesc) * fp8s.size() > L.fp8 || L.tables > ctx->slot_bytes)
-            return fail(RS_EINVAL, "internal: descriptor sizing");
+        at_reqs = align_up(at_pages + sizeof(int) * pagetab.size(), 16);
+        at_items = align_up(at_reqs + sizeof(ReqDesc) * reqs.size(), 16);
+        at_mitems = align_up(at_items + sizeof(AttnItem) * plan.items.size(), 16);
+        at_fp8 = align_up(at_mitems + sizeof(AttnMergeItem) * plan.merges.size(), 16);
+        staged_bytes = align_up(at_fp8 + sizeof(Fp8CacheDesc) * fp8s.size(), 16);
+        if (staged_bytes > L.tables || staged_bytes > ctx->slot_bytes) return fail(RS_EINVAL, "internal: descriptor sizing");
         memcpy(stage + at_reqs, reqs.data(), sizeof(ReqDesc) * reqs.size());
         memcpy(stage + at_items, plan.items.data(), sizeof(AttnItem) * plan.items.size());
         memcpy(stage + at_pages, pagetab.data(), sizeof(int) * pagetab.size());
         memcpy(stage + at_mitems, plan.merges.data(), sizeof(AttnMergeItem) * plan.merges.size());
         memcpy(stage + at_fp8, fp8s.data(), sizeof(Fp8CacheDesc) * fp8s.size());
-        staged_bytes = L.tables;
     }
     if (staged) {
         const int chunks16 = (int)(staged_bytes / 16);
