@@ -185,13 +185,19 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else int(t.data_ptr())
 
 
+_have_gpu = False
+
+
 def _stream_handle(stream) -> Optional[int]:
     import torch
     if isinstance(stream, int):
         return stream or None
     if stream is None:
-        if not torch.cuda.is_available():
-            return None  # GPU-less host: the call can only reach the library's argument checks
+        global _have_gpu
+        if not _have_gpu:
+            if not torch.cuda.is_available():
+                return None  # GPU-less host: the call can only reach the library's argument checks
+            _have_gpu = True
         stream = torch.cuda.current_stream()
     return int(stream.cuda_stream) or None
 
@@ -314,18 +320,30 @@ def _cache_set(kvs) -> CacheSet:
     return kvs if isinstance(kvs, CacheSet) else CacheSet(kvs)
 
 
+_bf16 = None   # torch.bfloat16, once torch is there
+
+
 def _rows(t, what: str, rows: int, width: int):
     """(address, distance between rows) of a bf16 tensor [rows, width] or [rows, heads, d] whose rows are contiguous."""
-    import torch
+    global _bf16
+    if _bf16 is None:
+        import torch
+        _bf16 = torch.bfloat16
     shape, stride = t.shape, t.stride()
+    if len(shape) == 2 and stride[1] == 1 and shape[1] == width and shape[0] == rows and t.dtype is _bf16:   # (the common case, in one go)
+        return t.data_ptr(), stride[0] if rows > 1 else width
     inner = 1
     for n, s in zip(reversed(shape[1:]), reversed(stride[1:])):
         if s != inner and n != 1:
             raise RsError(-1, f"the rows of {what} are not contiguous")
         inner *= n
-    if t.dtype is not torch.bfloat16 or not shape or shape[0] != rows or inner != width:
+    if t.dtype is not _bf16 or not shape or shape[0] != rows or inner != width:
         raise RsError(-1, f"{what} must be bfloat16 [{rows}, {width}]: {t.dtype} {list(shape)}")
     return t.data_ptr(), stride[0] if rows > 1 else width
+
+
+def _sum_of(a, n: int) -> int:
+    return a[0] if n == 1 else sum(a[:n])
 
 
 class PackedWeights:
@@ -644,8 +662,8 @@ class Context:
         cs, cfg = _cache_set(kvs), self.cfg
         rows, qw, kw = int(k.shape[0]), cfg.n_q_heads * cfg.head_dim, cfg.n_kv_heads * cfg.head_dim
         n = _ints(lens, len(cs), "lens")
-        if sum(n[: len(cs)]) != rows:
-            raise RsError(-1, f"lens add up to {sum(n[: len(cs)])}, k has {rows} rows")
+        if _sum_of(n, len(cs)) != rows:
+            raise RsError(-1, f"lens add up to {_sum_of(n, len(cs))}, k has {rows} rows")
         st, ps = _ints(starts, len(cs), "starts"), None
         if positions is not None:
             ps = _ints(positions.tolist() if hasattr(positions, "tolist") else positions, rows, "positions")
@@ -669,8 +687,8 @@ class Context:
         cs, width = _cache_set(kvs), self.cfg.n_q_heads * self.cfg.head_dim
         rows = int(q.shape[0])
         n = _ints(lens, len(cs), "lens")
-        if sum(n[: len(cs)]) != rows:
-            raise RsError(-1, f"lens add up to {sum(n[: len(cs)])}, q has {rows} rows")
+        if _sum_of(n, len(cs)) != rows:
+            raise RsError(-1, f"lens add up to {_sum_of(n, len(cs))}, q has {rows} rows")
         qp, ldq = _rows(q, "q", rows, width)
         op, ldo = _rows(out, "out", rows, width)
         _check(self.lib.rs_attend(self.handle, layer, cs.handles, n, len(cs), qp, ldq, op, ldo, scale, _ptr(workspace), workspace.numel(),
@@ -690,8 +708,8 @@ class Context:
         cs, cfg = _cache_set(kvs), self.cfg
         rows, width = int(q.shape[0]), cfg.n_q_heads * cfg.head_dim
         n = _ints(lens, len(cs), "lens")
-        if sum(n[: len(cs)]) != rows:
-            raise RsError(-1, f"lens add up to {sum(n[: len(cs)])}, q has {rows} rows")
+        if _sum_of(n, len(cs)) != rows:
+            raise RsError(-1, f"lens add up to {_sum_of(n, len(cs))}, q has {rows} rows")
         if chosen is not None and (chosen.dtype is not torch.int32 or not chosen.is_contiguous() or chosen.numel() != rows * cfg.n_kv_heads * n_blocks):
             raise RsError(-1, f"chosen must be contiguous int32 [{rows}, {cfg.n_kv_heads}, {n_blocks}]: {chosen.dtype} {list(chosen.shape)}")
         qp, ldq = _rows(q, "q", rows, width)

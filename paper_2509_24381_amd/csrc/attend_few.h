@@ -148,7 +148,9 @@ struct FewUnit {
     static constexpr int K_PATTERNS = (FP8 ? 64 : 32) * K_ROW / 1024 < LOADS ? (FP8 ? 64 : 32) * K_ROW / 1024 : LOADS;
 };
 
-template <int D, bool FP8, bool LIST, bool INLINE>
+// ONCE: nothing that is read is read again soon.
+constexpr int FEW_ONCE = 2;   // cache policy (nt)
+template <int D, bool FP8, bool LIST, bool ONCE, bool INLINE>
 __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a, std::conditional_t<INLINE, InlineTable, NoTable> tab) {
     typedef FewUnit<D, FP8> U;
     constexpr int KS = D / 32, DT = D / 16, NT = 4 / U::PER, DTU = DT / U::PER;   // sub-tiles of a K unit, feature blocks of a V unit
@@ -248,7 +250,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
         for (int i = 0; i < U::LOADS; ++i) {
             const uint32_t from = keys ? k_src[i % U::K_PATTERNS] : v_src;   // (named: template-dependent arguments of the builtin break the host-side stub)
             const int further = h % U::PER * U::BYTES + (keys ? i / U::K_PATTERNS * U::K_PATTERNS : i) * 1024;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)(uintptr_t)(uint32_t)(uintptr_t)(to + i * 1024), 16, from, further, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)(uintptr_t)(uint32_t)(uintptr_t)(to + i * 1024), 16, from, further, 0, ONCE ? FEW_ONCE : 0);
         }
     };
     // (the compiler does not see LDS written by DMA, nor may it move a refill above the reads of what it overwrites)

@@ -28,6 +28,10 @@ struct rs_rotary {
 namespace {
 
 constexpr int FEW_ROWS = 64;       // stacked rows of a request up to which it goes to attend_few_kernel
+// Caches that one call reads once are loaded with the streaming hint, unless they are so small that the L2s may still have them from a call
+// before.  us with / without it, behind a fill of 1 GB: 8 MB 14.6 / 15.6, 35 MB 19.6 / 26.6, 141 MB 38.3 / 69.5; call after call on the
+// same caches: 4 MB 15.7 / 14.6, 8 MB 20.2 / 20.4, 141 MB 53.3 / 54.5.
+constexpr size_t FEW_ONCE_BYTES = (size_t)8 << 20;
 constexpr int FEW_PLACES = 2;      // workgroups of attend_few_kernel that a compute unit holds
 constexpr size_t SLOT_ROWS = 65536;   // rows there is room for in the slots of split key ranges
 constexpr size_t SELECT_LDS = (size_t)SELECT_MAX_BLOCKS * 4;
@@ -198,8 +202,12 @@ AttendLayout attend_layout(const rs_layer_cfg& f, int max_rows, int max_requests
 size_t expansion_bytes(const rs_ctx* c, long tokens) { return (size_t)2 * align_up((size_t)tokens, 64) * c->kv_dim * 2; }
 
 // ---------------------------------------------------------------- few rows
-// Parts of the key ranges.  A part's cost is its tiles; what is minimised is the time of the longest, and, with more items than run at
-// once, the share of each place plus half a part, and two tiles for joining.
+// Parts of the key ranges, of `len` tiles at most.  Estimated in tiles of a place (a workgroup's room on a compute unit) when all places stream:
+// an item costs 1.5 beside its tiles, joining 2.  With no more items than places the longest ends last, but the fewer are left the
+// faster they stream: a tile then takes 0.66 of one (more where several wavefronts need every tile: 16 rows each).  With more, the last
+// ones start late: a share of the longest comes on top.  us a pass, parts of 4 / 8 / 16 / 24 / 48 tiles: 64 requests on up to 8000 tokens
+// 100.5 / 93.8 / 88.7 / 92.2 / 90.1; 16 on up to 32000, 8 bits, 82.8 / 77.6 / 70.6 / 67.6 / 61.1; 24 of 3 tokens on up to 6000, 8 query
+// heads per KV head, 77.5 / 73.2 / 72.4 / 87.2 / 99.7.
 struct FewRequest {
     int kv, row0, T;       // index into kvs, first row, rows
     int units, tiles;      // items per part, tiles
@@ -217,14 +225,15 @@ void plan_few(std::vector<FewRequest>& reqs, int places, size_t slots) {
     int best_len = longest;
     for (int len = FEW_WAVES; ; len = std::min(longest, len + std::max(1, len / 8))) {
         long items = 0, split = 0;
-        int most = 0;
+        double most = 0.0;
         for (const FewRequest& r : reqs) {
             const int p = std::min((r.tiles + len - 1) / len, FEW_MAX_PARTS);
             items += (long)r.units * p;
             if (p > 1) split += (long)r.units * p * r.row_blocks;
-            most = std::max(most, (r.tiles + p - 1) / p);
+            most = std::max(most, ((r.tiles + p - 1) / p) * (r.row_blocks == 1 ? 0.66 : r.row_blocks == 2 ? 0.85 : 1.1));
         }
-        const double cost = (items <= places ? most : std::max<double>(most, (double)total / places + 0.5 * most)) + (split ? 2.0 : 0.0);
+        const double share = (double)total / places;
+        const double cost = (items <= places ? std::max(share, most) + 1.5 : share + 1.5 * items / places + 0.5 * most) + (split ? 2.0 : 0.0);
         if ((size_t)split <= slots && cost < best) {
             best = cost;
             best_len = len;
@@ -277,19 +286,22 @@ size_t few_table_words(const rs_ctx*, rs_kv* const* kvs, const std::vector<FewRe
 }
 
 template <bool LIST>
-rs_status launch_few(const rs_ctx* ctx, bool fp8, const FewArgs& a, uint32_t items, uint32_t units, bool split, const InlineTable* tab, hipStream_t st) {
+rs_status launch_few(const rs_ctx* ctx, bool fp8, bool once, const FewArgs& a, uint32_t items, uint32_t units, bool split, const InlineTable* tab, hipStream_t st) {
     for_kind(ctx, fp8, [&](auto d, auto f8) {
         constexpr int D = decltype(d)::value;
         constexpr bool FP8 = decltype(f8)::value;
-        if constexpr (!LIST) {
-            if (tab) {
-                hipLaunchKernelGGL((attend_few_kernel<D, FP8, false, true>), dim3(items), dim3(64 * FEW_WAVES), 0, st, a, *tab);
-                if (split) hipLaunchKernelGGL((few_merge_kernel<D, false, true>), dim3(units, D / 32), dim3(256), 0, st, a, *tab);
-                return;
-            }
+        if constexpr (LIST) {
+            hipLaunchKernelGGL((attend_few_kernel<D, FP8, true, false, false>), dim3(items), dim3(64 * FEW_WAVES), 0, st, a, NoTable{});
+            if (split) hipLaunchKernelGGL((few_merge_kernel<D, true, false>), dim3(units, D / 32), dim3(256), 0, st, a, NoTable{});
+        } else if (tab) {
+            if (once) hipLaunchKernelGGL((attend_few_kernel<D, FP8, false, true, true>), dim3(items), dim3(64 * FEW_WAVES), 0, st, a, *tab);
+            else hipLaunchKernelGGL((attend_few_kernel<D, FP8, false, false, true>), dim3(items), dim3(64 * FEW_WAVES), 0, st, a, *tab);
+            if (split) hipLaunchKernelGGL((few_merge_kernel<D, false, true>), dim3(units, D / 32), dim3(256), 0, st, a, *tab);
+        } else {
+            if (once) hipLaunchKernelGGL((attend_few_kernel<D, FP8, false, true, false>), dim3(items), dim3(64 * FEW_WAVES), 0, st, a, NoTable{});
+            else hipLaunchKernelGGL((attend_few_kernel<D, FP8, false, false, false>), dim3(items), dim3(64 * FEW_WAVES), 0, st, a, NoTable{});
+            if (split) hipLaunchKernelGGL((few_merge_kernel<D, false, false>), dim3(units, D / 32), dim3(256), 0, st, a, NoTable{});
         }
-        hipLaunchKernelGGL((attend_few_kernel<D, FP8, LIST, false>), dim3(items), dim3(64 * FEW_WAVES), 0, st, a, NoTable{});
-        if (split) hipLaunchKernelGGL((few_merge_kernel<D, LIST, false>), dim3(units, D / 32), dim3(256), 0, st, a, NoTable{});
     });
     RS_HIP(hipGetLastError());
     return RS_OK;
@@ -591,8 +603,10 @@ rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, 
     FewTable ft;
     InlineTable tab;
     bool inline_table = false;
-    size_t few_words = 0;
+    size_t few_words = 0, few_bytes = 0;   // few_bytes: of the keys and values they read
     if (!few.empty()) {
+        for (const FewRequest& r : few) few_bytes += (size_t)r.tiles * 128 * ctx->kv_dim * (fp8 ? 1 : 2);
+
         plan_few(few, FEW_PLACES * ctx->n_cu, SLOT_ROWS / 16);
         a.n_req = (int)few.size();
         a.hkv = f.n_kv_heads; a.g = ctx->group;
@@ -676,7 +690,7 @@ rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, 
         if ((s = ring_commit(ctx, st)) != RS_OK) return s;
     }
     if (!few.empty() &&
-        (s = launch_few<false>(ctx, fp8, a, ft.items, ft.units, ft.any_split, inline_table ? &tab : nullptr, st)) != RS_OK)
+        (s = launch_few<false>(ctx, fp8, few_bytes >= FEW_ONCE_BYTES, a, ft.items, ft.units, ft.any_split, inline_table ? &tab : nullptr, st)) != RS_OK)
         return s;
     if (!chunks) return RS_OK;
     const ReqDesc* const d_reqs = reinterpret_cast<const ReqDesc*>(ws + at_reqs);
@@ -853,7 +867,7 @@ rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int*
     a.chosen = list;
     a.n_blocks = n_blocks;
     a.list_parts = parts;
-    return launch_few<true>(ctx, fp8, a, (uint32_t)(units * parts), (uint32_t)(units * rbn), parts > 1, nullptr, st);
+    return launch_few<true>(ctx, fp8, false, a, (uint32_t)(units * parts), (uint32_t)(units * rbn), parts > 1, nullptr, st);
 }
 
 }  // extern "C"
