@@ -467,7 +467,6 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
 // features, a quarter of the parts per 64 threads (16 rows x 4 chunks of 8 features).
 template <int D, bool LIST, bool INLINE>
 __global__ __launch_bounds__(256) void few_merge_kernel(FewArgs a, std::conditional_t<INLINE, InlineTable, NoTable> tab) {
-    constexpr int MAXP = FEW_MAX_PARTS / 4;
     __shared__ float m_sh[4][16];
     __shared__ float red[4][64][9];
     const uint32_t* const table = table_of<INLINE>(tab, a.table);
@@ -503,30 +502,51 @@ __global__ __launch_bounds__(256) void few_merge_kernel(FewArgs a, std::conditio
     const int group = threadIdx.x >> 6, row = (threadIdx.x & 63) >> 2, f0 = blockIdx.y * 32 + (threadIdx.x & 3) * 8, i = b * 16 + row;
     const float* const base = a.slots + (size_t)(rq.slot0 + unit * parts * rbn + b) * FewSlot<D>::FLOATS;
     const size_t next = (size_t)rbn * FewSlot<D>::FLOATS;
-    float mp[MAXP], M = -INFINITY, L = 0.0f, o[8] = {};
+    // four parts at a time, all their loads in flight together, on to a running reference M
+    float M = -INFINITY, L = 0.0f, o[8] = {};
+    for (int p0 = group; p0 < parts; p0 += 16) {
+        float mp[4], lp[4];
+        f32x4 x[4], y[4];
 #pragma unroll
-    for (int k = 0; k < MAXP; ++k) {
-        const int p = k * 4 + group;
-        mp[k] = p < parts ? base[p * next + (size_t)16 * D + row] : -INFINITY;
-        M = fmaxf(M, mp[k]);
+        for (int k = 0; k < 4; ++k) {
+            const float* const sp = base + (size_t)min(p0 + 4 * k, parts - 1) * next;
+            mp[k] = sp[(size_t)16 * D + row];
+            lp[k] = sp[(size_t)16 * (D + 1) + row];
+            x[k] = *reinterpret_cast<const f32x4*>(sp + (size_t)row * D + f0);
+            y[k] = *reinterpret_cast<const f32x4*>(sp + (size_t)row * D + f0 + 4);
+        }
+        float big = M;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (p0 + 4 * k < parts) big = fmaxf(big, mp[k]);
+        const float alpha = M == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(M - big);
+        M = big;
+        if (L != 0.0f) {   // (sums of nothing stay, whatever the reference)
+            L *= alpha;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] *= alpha;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            // (a part none of whose keys count has a row sum of zero and no reference)
+            const float w = p0 + 4 * k >= parts || lp[k] == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(mp[k] - M);
+            if (p0 + 4 * k >= parts) continue;
+            L += w * lp[k];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                o[e] += w * x[k][e];
+                o[4 + e] += w * y[k][e];
+            }
+        }
     }
     if ((threadIdx.x & 3) == 0) m_sh[group][row] = M;
     __syncthreads();
-    M = fmaxf(fmaxf(m_sh[0][row], m_sh[1][row]), fmaxf(m_sh[2][row], m_sh[3][row]));
+    {
+        const float big = fmaxf(fmaxf(m_sh[0][row], m_sh[1][row]), fmaxf(m_sh[2][row], m_sh[3][row]));
+        const float w = L == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(M - big);
+        L *= w;
 #pragma unroll
-    for (int k = 0; k < MAXP; ++k) {
-        const int p = k * 4 + group;
-        if (p >= parts) continue;
-        const float* const sp = base + p * next;
-        // (a part none of whose keys count has a row sum of zero and no reference)
-        const float lp = sp[(size_t)16 * (D + 1) + row], w = lp == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(mp[k] - M);
-        L += w * lp;
-        const f32x4 x = *reinterpret_cast<const f32x4*>(sp + (size_t)row * D + f0), y = *reinterpret_cast<const f32x4*>(sp + (size_t)row * D + f0 + 4);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            o[e] += w * x[e];
-            o[4 + e] += w * y[e];
-        }
+        for (int e = 0; e < 8; ++e) o[e] *= w;
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) red[group][threadIdx.x & 63][e] = o[e];

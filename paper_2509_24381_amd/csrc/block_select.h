@@ -104,8 +104,10 @@ __global__ __launch_bounds__(256) void key_bounds_kernel(int n_req, int hkv, int
 //     that order like the scores, into LDS;
 //  3. a team per token finds the score that the last selected block has, digit by digit of the keys' range (a histogram in LDS per
 //     digit: integers, in any order the same), and writes the blocks down in ascending order.
-// WAVES = 4: four tokens, a wavefront each; bound by the latency of its few dependent steps, so that many are needed at once.  WAVES = 16: one
-// token, for calls of few, whose score step reads the bounds of a long cache (8 KB per KV head and 32 blocks at d = 128).
+// With many tokens a workgroup has four, a wavefront each, and takes all three steps.  With few (WIDE) it has one, and where that has more
+// blocks than a workgroup scores at once, the first two steps are a launch of their own, of a workgroup per 256 blocks: a compute unit alone
+// gets 33 bytes per ns, 16 us for the bounds of 2046 blocks.  (One launch, the last workgroup to finish selecting: the fence that makes
+// keys visible across the chip takes longer than a second launch, 7 us.)
 struct SelectReq {          // 64 bytes
     uint64_t codes, units;
     int32_t room;
@@ -117,8 +119,10 @@ struct SelectArgs {
     int n_req, hkv, g, halvings;
     const bf16* q;
     long ld_q;
-    int tokens;             // tokens of a workgroup: 1 with WAVES = 16, else at most 4
-    int blocks;             // keys there is room for per token in LDS
+    int tokens;             // tokens of a workgroup: 1 if WIDE, else at most 4
+    int blocks;             // keys there is room for per token, a multiple of 4
+    int split;              // WIDE: workgroups that share a token's blocks in the score step
+    uint32_t* shared_keys;  // WIDE, split > 1: the keys between the launches, [row][KV head][blocks]
     int n_blocks, n_first, n_last;
     int* chosen;
     // the attention kernel's table, from the staging buffer to the workspace: workgroups (x >= groups, y = 0) copy it
@@ -134,14 +138,14 @@ RS_DEVICE uint32_t key_of_score(float s) {
 }
 
 // What a team shares in LDS.
-template <int WAVES>
+template <int TEAM>
 struct SelectTeam {
     uint32_t hist[256];
-    uint32_t digit, left;            // of a digit's search
-    uint32_t low[WAVES], high[WAVES];
+    uint32_t digit, left, done;      // of a digit's search
+    uint32_t low[TEAM], high[TEAM];
 };
 
-// The take-th largest of key[lo .. hi), 0 < take < hi - lo; *equals: how many of those equal to it belong to the `take`.  TEAM wavefronts.
+// A key that exactly `take` of key[lo .. hi) are above, 0 < take < hi - lo, but for *equals of those equal to it.  TEAM wavefronts.
 template <int TEAM>
 RS_DEVICE uint32_t cut_of_keys(const uint32_t* key, int lo, int hi, int take, SelectTeam<TEAM>& sh, int* equals) {
     const int lane = threadIdx.x & 63, member = TEAM == 1 ? lane : (int)threadIdx.x, wave = TEAM == 1 ? 0 : (int)threadIdx.x >> 6;
@@ -203,8 +207,10 @@ RS_DEVICE uint32_t cut_of_keys(const uint32_t* key, int lo, int hi, int take, Se
                         rest -= count[i];
                         d = i - 1;
                     }
+                const uint32_t in_digit = d == 3 ? h.w : d == 2 ? h.z : d == 1 ? h.y : h.x;
                 sh.digit = (uint32_t)lane * 4 + d;
                 sh.left = rest;
+                sh.done = rest == in_digit;   // (all of that digit belong: nothing below it matters)
             }
         }
         meet();
@@ -212,35 +218,68 @@ RS_DEVICE uint32_t cut_of_keys(const uint32_t* key, int lo, int hi, int take, Se
         left = sh.left;
         top = shift;
         first = false;
+        const bool done = sh.done != 0;
         meet();
+        if (done && top > 0) {   // all from the digit's smallest key on; (prefix << top is not 0: some keys are left out)
+            *equals = 0;
+            return low + (prefix << top) - 1u;
+        }
     }
     *equals = (int)left;
     return low + prefix;
 }
 
-template <int D, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void block_select_kernel(SelectArgs a, InlineTable tab) {
-    constexpr int TEAM = WAVES == 16 ? 16 : 1, TEAMS = WAVES / TEAM, KK = 2 * D / 64;
+constexpr int SELECT_U = 4;                            // groups of 16 blocks that a wavefront has in flight
+constexpr int SELECT_ROUND = 4 * 16 * SELECT_U;        // blocks that a workgroup scores at a time
+enum SelectSteps { SELECT_ALL = 0, SELECT_SCORES = 1, SELECT_FROM_SCORES = 2 };
+template <int D, bool WIDE, int STEPS>
+__global__ __launch_bounds__(STEPS == SELECT_FROM_SCORES ? 1024 : 256) void block_select_kernel(SelectArgs a, InlineTable tab) {
+    static_assert(WIDE || STEPS == SELECT_ALL, "only few tokens take two launches");
+    constexpr int WAVES = STEPS == SELECT_FROM_SCORES ? 16 : 4, TEAM = WIDE ? WAVES : 1, TEAMS = WAVES / TEAM, KK = 2 * D / 64, U = SELECT_U;
     extern __shared__ __attribute__((aligned(16))) uint32_t keys[];   // [tokens][blocks]
     __shared__ __attribute__((aligned(16))) int8_t u[16][2 * D];
     __shared__ __attribute__((aligned(16))) SelectTeam<TEAM> team_sh[TEAMS];
     __shared__ uint32_t chunk_more[TEAM == 1 ? 1 : SELECT_MAX_BLOCKS / 64], chunk_equal[TEAM == 1 ? 1 : SELECT_MAX_BLOCKS / 64];
     const uint32_t* const table = tab.w;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = blockIdx.y;
-    if ((int)blockIdx.x >= a.groups) {
+    if (STEPS != SELECT_FROM_SCORES && (int)blockIdx.x >= a.groups) {
         const int i = ((int)blockIdx.x - a.groups) * 64 * WAVES + (int)threadIdx.x;
         if (h == 0 && i < a.copy_chunks) a.copy_to[i] = a.copy_from[i];
         return;
     }
-    const int req = request_of(table, a.n_req, blockIdx.x);
+    const int split = STEPS == SELECT_SCORES ? a.split : 1, share = (int)blockIdx.x % split, item = (int)blockIdx.x / split;
+    const int req = request_of(table, a.n_req, (uint32_t)item);
     const SelectReq rq = reinterpret_cast<const SelectReq*>(table + table_reqs_at(a.n_req))[req];
-    const int t0 = (int)(blockIdx.x - table[req]) * a.tokens, nt = min(a.tokens, rq.T - t0);
+    const int t0 = (item - (int)table[req]) * a.tokens, nt = min(a.tokens, rq.T - t0);
     const int b_last = (rq.P + t0 + nt - 1) / 64;          // own block of the last token
     // blocks that can need a score
     const int s0 = min(a.n_first, b_last), s1 = max(s0, b_last + 1 - a.n_last);
     const bool scored = b_last + 1 > a.n_blocks && s1 > s0;   // (else every token takes all it has, or none but the forced ones)
-    if (scored) {
+    uint32_t* const shared = STEPS == SELECT_ALL ? nullptr : a.shared_keys + ((size_t)(rq.row0 + t0) * a.hkv + h) * a.blocks;
+    uint32_t* const to = STEPS == SELECT_SCORES ? shared : keys;   // where the scores' keys go
+    if (STEPS == SELECT_FROM_SCORES && scored) {
+        for (int i = threadIdx.x * 4; i < s1 - s0; i += 64 * WAVES * 4) *reinterpret_cast<uint4*>(&keys[i]) = *reinterpret_cast<const uint4*>(&shared[i]);
+        __syncthreads();
+    }
+    if (STEPS != SELECT_FROM_SCORES && scored) {
         constexpr int W = D / 64;   // features of a lane: W lane ..
+        const int r = lane & 15, c = lane >> 4;
+        const int8_t* const codes = reinterpret_cast<const int8_t*>(rq.codes) + (size_t)h * rq.room * 2 * D;
+        const float* const units = reinterpret_cast<const float*>(rq.units) + (size_t)h * rq.room;
+        i32x4 x[U][KK];
+        float unit[U][4];
+        const auto load = [&](int b) RS_INLINE {   // bounds of the wavefront's blocks b ..
+#pragma unroll
+            for (int v = 0; v < U; ++v) {
+                const int8_t* const src = codes + (size_t)min(b + v * 16 + r, s1 - 1) * 2 * D + c * 16;
+#pragma unroll
+                for (int k = 0; k < KK; ++k) x[v][k] = *reinterpret_cast<const i32x4*>(src + k * 64);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) unit[v][e] = units[min(b + v * 16 + c * 4 + e, s1 - 1)];
+            }
+        };
+        int b = s0 + share * SELECT_ROUND + wave * 16 * U;
+        load(b);   // (under way while the queries become codes)
         for (int t = wave; t < 16; t += WAVES) {
             int p[W] = {}, n[W] = {};
             if (t < nt) {
@@ -285,24 +324,10 @@ __global__ __launch_bounds__(64 * WAVES) void block_select_kernel(SelectArgs a, 
             }
         }
         __syncthreads();
-        const int r = lane & 15, c = lane >> 4;
         i32x4 uf[KK];
 #pragma unroll
         for (int k = 0; k < KK; ++k) uf[k] = *reinterpret_cast<const i32x4*>(&u[r][k * 64 + c * 16]);
-        const int8_t* const codes = reinterpret_cast<const int8_t*>(rq.codes) + (size_t)h * rq.room * 2 * D;
-        const float* const units = reinterpret_cast<const float*>(rq.units) + (size_t)h * rq.room;
-        constexpr int U = 4;   // groups of 16 blocks in flight
-        for (int b = s0 + wave * 16 * U; b < s1; b += WAVES * 16 * U) {
-            i32x4 x[U][KK];
-            float unit[U][4];
-#pragma unroll
-            for (int v = 0; v < U; ++v) {
-                const int8_t* const src = codes + (size_t)min(b + v * 16 + r, s1 - 1) * 2 * D + c * 16;
-#pragma unroll
-                for (int k = 0; k < KK; ++k) x[v][k] = *reinterpret_cast<const i32x4*>(src + k * 64);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) unit[v][e] = units[min(b + v * 16 + c * 4 + e, s1 - 1)];
-            }
+        while (b < s1) {
 #pragma unroll
             for (int v = 0; v < U; ++v) {
                 i32x4 dot = {0, 0, 0, 0};
@@ -311,12 +336,15 @@ __global__ __launch_bounds__(64 * WAVES) void block_select_kernel(SelectArgs a, 
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {   // block b + 16 v + 4 c + e, token r
                     const int block = b + v * 16 + c * 4 + e;
-                    if (r < nt && block < s1) keys[r * a.blocks + block - s0] = key_of_score((float)dot[e] * unit[v][e]);
+                    if (r < nt && block < s1) to[r * a.blocks + block - s0] = key_of_score((float)dot[e] * unit[v][e]);
                 }
             }
+            b += split * SELECT_ROUND;
+            if (b < s1) load(b);
         }
         __syncthreads();
     }
+    if constexpr (STEPS == SELECT_SCORES) return;
     const unsigned long long below = lane == 0 ? 0ull : ~0ull >> (64 - lane);   // the lanes before this one
     for (int t = TEAM == 1 ? wave : 0; t < nt; t += TEAMS) {
         const int own = (rq.P + t0 + t) / 64;

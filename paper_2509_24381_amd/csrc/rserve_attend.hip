@@ -34,6 +34,8 @@ constexpr int FEW_ROWS = 64;       // stacked rows of a request up to which it g
 constexpr size_t FEW_ONCE_BYTES = (size_t)8 << 20;
 constexpr int FEW_PLACES = 2;      // workgroups of attend_few_kernel that a compute unit holds
 constexpr size_t SLOT_ROWS = 65536;   // rows there is room for in the slots of split key ranges
+// Tokens times KV heads up to which workgroups share a token's blocks (block_select_kernel).
+constexpr size_t SELECT_WIDE_UNITS = 256;
 constexpr size_t SELECT_LDS = (size_t)SELECT_MAX_BLOCKS * 4;
 
 // ---- checks that all calls share; *rows_out: the sum of lens (null lens: none)
@@ -179,7 +181,7 @@ rs_status launch_bounds(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* fi
 // ---------------------------------------------------------------- workspace
 struct AttendLayout {
     size_t few, reqs, items, pagetab, mitems, fp8, tables;   // descriptors: sizes, and their sum
-    size_t slots_at, chosen_at, split_at, total;             // offsets behind them
+    size_t slots_at, keys_at, chosen_at, split_at, total;   // offsets behind them
 };
 AttendLayout attend_layout(const rs_layer_cfg& f, int max_rows, int max_requests, int n_blocks) {
     const size_t rows = std::max(max_rows, 1), reqs = std::max(max_requests, 1), g = f.n_q_heads / f.n_kv_heads;
@@ -193,7 +195,8 @@ AttendLayout attend_layout(const rs_layer_cfg& f, int max_rows, int max_requests
     w.fp8 = align_up(sizeof(Fp8CacheDesc) * reqs, 256);
     w.tables = w.few + w.reqs + w.items + w.pagetab + w.mitems + w.fp8;
     w.slots_at = w.tables;
-    w.chosen_at = w.slots_at + align_up(SLOT_ROWS * (f.head_dim + 2) * 4, 256);
+    w.keys_at = w.slots_at + align_up(SLOT_ROWS * (f.head_dim + 2) * 4, 256);
+    w.chosen_at = w.keys_at + align_up(n_blocks > 0 ? std::min<size_t>(rows * f.n_kv_heads, SELECT_WIDE_UNITS) * align_up(f.max_pos / 64 + 1, 4) * 4 : 0, 256);
     w.split_at = w.chosen_at + align_up(n_blocks > 0 ? rows * f.n_kv_heads * n_blocks * 4 : 0, 256);
     w.total = w.split_at;
     if (n_blocks == 0 && rows * g > FEW_ROWS) w.total += align_up((size_t)ATT_SPLIT_SLOTS * 32 * ATT_WAVES * (f.head_dim + 2) * 4, 256);
@@ -772,8 +775,9 @@ rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int*
     char* const ws = reinterpret_cast<char*>(workspace);
     const bool fp8 = kvs[0]->fp8;
     if (!ctx->select_ready) {   // first use on this context: opt in to the LDS size once
-        for (const void* k : {(const void*)block_select_kernel<64, 4>, (const void*)block_select_kernel<64, 16>, (const void*)block_select_kernel<128, 4>,
-                              (const void*)block_select_kernel<128, 16>})
+        for (const void* k : {(const void*)block_select_kernel<64, false, SELECT_ALL>, (const void*)block_select_kernel<64, true, SELECT_ALL>,
+                              (const void*)block_select_kernel<64, true, SELECT_FROM_SCORES>, (const void*)block_select_kernel<128, false, SELECT_ALL>,
+                              (const void*)block_select_kernel<128, true, SELECT_ALL>, (const void*)block_select_kernel<128, true, SELECT_FROM_SCORES>})
             RS_HIP(hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)SELECT_LDS));
         ctx->select_ready = true;
     }
@@ -813,15 +817,17 @@ rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int*
     sa.hkv = f.n_kv_heads; sa.g = ctx->group;
     for (int x = 1; x < ctx->group; x *= 2) ++sa.halvings;
     sa.q = (const bf16*)q; sa.ld_q = ld_q;
-    sa.blocks = longest;
+    sa.blocks = (int)align_up(longest, 4);
     sa.n_blocks = n_blocks; sa.n_first = n_first; sa.n_last = n_last;
     sa.chosen = list;
-    const bool wide = units <= ctx->n_cu;   // few tokens: sixteen wavefronts score one token's blocks
+    const bool wide = (size_t)units <= SELECT_WIDE_UNITS;
     sa.tokens = wide ? 1 : (int)std::min<size_t>(4, SELECT_LDS / ((size_t)longest * 4));
     sa.copy_from = reinterpret_cast<const uint4*>(ctx->pinned_dev[slot]);
     sa.copy_to = reinterpret_cast<uint4*>(ws);
     sa.copy_chunks = copy_chunks;
-    const int threads = wide ? 1024 : 256;
+    sa.split = wide ? std::min((longest + SELECT_ROUND - 1) / SELECT_ROUND, std::max(1, 2 * ctx->n_cu / units)) : 1;
+    sa.shared_keys = reinterpret_cast<uint32_t*>(ws + L.keys_at);
+    constexpr int threads = 256;
     constexpr int WINDOW = TABLE_WORDS / 20;   // requests whose descriptors the kernel arguments hold
     for (size_t i0 = 0; i0 < reqs.size(); i0 += WINDOW) {
         const int n = (int)std::min<size_t>(WINDOW, reqs.size() - i0);
@@ -841,19 +847,22 @@ rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int*
             groups += (uint32_t)((r.T + sa.tokens - 1) / sa.tokens);
         }
         sa.n_req = n;
-        sa.groups = (int)groups;
-        const dim3 grid(groups + (i0 == 0 ? (copy_chunks + threads - 1) / threads : 0), f.n_kv_heads);
+        const unsigned copying = i0 == 0 ? (unsigned)((copy_chunks + threads - 1) / threads) : 0u;
         const size_t lds = (size_t)sa.tokens * sa.blocks * 4;
-        const auto select = [&](auto d, auto waves) {
-            hipLaunchKernelGGL((block_select_kernel<decltype(d)::value, decltype(waves)::value>), grid, dim3(64 * decltype(waves)::value), lds, st, sa, tab);
+        const auto select = [&](auto d) {
+            constexpr int D = decltype(d)::value;
+            if (sa.split > 1) {
+                sa.groups = (int)groups * sa.split;
+                hipLaunchKernelGGL((block_select_kernel<D, true, SELECT_SCORES>), dim3(groups * sa.split + copying, f.n_kv_heads), dim3(threads), 0, st, sa, tab);
+                hipLaunchKernelGGL((block_select_kernel<D, true, SELECT_FROM_SCORES>), dim3(groups, f.n_kv_heads), dim3(1024), lds, st, sa, tab);
+                return;
+            }
+            sa.groups = (int)groups;
+            if (wide) hipLaunchKernelGGL((block_select_kernel<D, true, SELECT_ALL>), dim3(groups + copying, f.n_kv_heads), dim3(threads), lds, st, sa, tab);
+            else hipLaunchKernelGGL((block_select_kernel<D, false, SELECT_ALL>), dim3(groups + copying, f.n_kv_heads), dim3(threads), lds, st, sa, tab);
         };
-        if (f.head_dim == 128) {
-            if (wide) select(std::integral_constant<int, 128>{}, std::integral_constant<int, 16>{});
-            else select(std::integral_constant<int, 128>{}, std::integral_constant<int, 4>{});
-        } else {
-            if (wide) select(std::integral_constant<int, 64>{}, std::integral_constant<int, 16>{});
-            else select(std::integral_constant<int, 64>{}, std::integral_constant<int, 4>{});
-        }
+        if (f.head_dim == 128) select(std::integral_constant<int, 128>{});
+        else select(std::integral_constant<int, 64>{});
         RS_HIP(hipGetLastError());
         if (i0 == 0 && (s = ring_commit(ctx, st)) != RS_OK) return s;
     }
