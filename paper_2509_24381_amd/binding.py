@@ -185,20 +185,21 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else int(t.data_ptr())
 
 
-_have_gpu = False
+_raw_stream = None   # handle of a device's current stream, once a GPU has been seen
 
 
 def _stream_handle(stream) -> Optional[int]:
-    import torch
-    if isinstance(stream, int):
-        return stream or None
+    global _raw_stream
     if stream is None:
-        global _have_gpu
-        if not _have_gpu:
+        import torch
+        if _raw_stream is None:
             if not torch.cuda.is_available():
                 return None  # GPU-less host: the call can only reach the library's argument checks
-            _have_gpu = True
-        stream = torch.cuda.current_stream()
+            # (the current stream's handle without the object around it, where torch has that: 0.4 us instead of 2.9)
+            _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+        return _raw_stream(torch.cuda.current_device()) or None
+    if isinstance(stream, int):
+        return stream or None
     return int(stream.cuda_stream) or None
 
 

@@ -75,8 +75,9 @@ RS_DEVICE void turn_pairs(int j, int rd, const float2* cs, bf16x8& x, bf16x8& y)
 }
 
 constexpr int APPEND_FEW = 8;   // up to this many tokens of a block the values are stored one by one
-template <int D, bool FP8, bool INTERLEAVED>
-__global__ __launch_bounds__(256) void rope_append_kernel(AppendArgs a, InlineTable tab) {
+struct SmallTable { uint32_t w[112]; };   // the table of a few requests: a launch of 4 KB of arguments takes the host 1.3 us more
+template <int D, bool FP8, bool INTERLEAVED, class Tab>
+__global__ __launch_bounds__(256) void rope_append_kernel(AppendArgs a, Tab tab) {
     constexpr int TASKS = D / 16, EL = FP8 ? 1 : 2;
     const uint32_t* const table = tab.w;
     const AppendItem it = reinterpret_cast<const AppendItem*>(table)[blockIdx.x];
@@ -103,36 +104,65 @@ __global__ __launch_bounds__(256) void rope_append_kernel(AppendArgs a, InlineTa
     const int h = blockIdx.y;
     char* const kt = reinterpret_cast<char*>(it.k + (uint64_t)h * it.head_bytes);
     char* const vt = reinterpret_cast<char*>(it.v + (uint64_t)h * it.head_bytes);
-    for (int i = threadIdx.x; i < n * TASKS; i += 256) {   // keys
-        const int t = i / TASKS, j = i % TASKS;
-        int fa, fb;
-        pair_task<INTERLEAVED>(j, a.rd, fa, fb);
-        const bf16* src = a.k + (size_t)(it.row0 + t) * a.ld_k + h * D;
-        bf16x8 x = as_bf16x8(ld_global_16(src + fa)), y = as_bf16x8(ld_global_16(src + fb));
-        turn_pairs<INTERLEAVED>(j, a.rd, angles(t), x, y);
-        char* const dst = kt + (size_t)(slot + t) * D * EL;
-        if constexpr (FP8) {
-            *reinterpret_cast<uint2*>(dst + fa) = e4m3_from_bf16x8(x, it.k_inv);
-            *reinterpret_cast<uint2*>(dst + fb) = e4m3_from_bf16x8(y, it.k_inv);
-        } else {
-            st_global_16(dst + fa * 2, as_uint4(x));
-            st_global_16(dst + fb * 2, as_uint4(y));
-        }
-    }
+    const bf16* const k0 = a.k + (size_t)it.row0 * a.ld_k + h * D;
     const bf16* const v0 = a.v + (size_t)it.row0 * a.ld_v + h * D;
     const int end = slot + n;
-    const auto store_one = [&](int d, int place, bf16 v) RS_INLINE {
-        if constexpr (FP8) reinterpret_cast<uint8_t*>(vt)[d * 64 + place] = (uint8_t)(e4m3_pair(bf16_to_f32(v) * it.v_inv, 0.0f) & 0xffu);
-        else reinterpret_cast<bf16*>(vt)[d * 64 + place] = v;
+    const bool turned = n > APPEND_FEW || it.zero_tail;   // values go through LDS
+    __shared__ __attribute__((aligned(16))) bf16 tile[64][D + 8];
+    // all of a thread's loads first: its 16-byte chunks of values, its tasks of the keys
+    constexpr int VN = 64 * (D / 8) / 256, KN = (64 * TASKS + 255) / 256;
+    uint4 v[4], x[2], y[2];
+    static_assert(VN <= 4 && KN <= 2, "head dim 128 at most");
+    if (turned) {
+#pragma unroll
+        for (int j = 0; j < VN; ++j) {
+            const int i = j * 256 + (int)threadIdx.x;
+            if (i < n * (D / 8)) v[j] = ld_global_16(v0 + (size_t)(i / (D / 8)) * a.ld_v + i % (D / 8) * 8);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < KN; ++j) {
+        const int i = j * 256 + (int)threadIdx.x;
+        if (i < n * TASKS) {
+            int fa, fb;
+            pair_task<INTERLEAVED>(i % TASKS, a.rd, fa, fb);
+            x[j] = ld_global_16(k0 + (size_t)(i / TASKS) * a.ld_k + fa);
+            y[j] = ld_global_16(k0 + (size_t)(i / TASKS) * a.ld_k + fb);
+        }
+    }
+    if (turned) {
+#pragma unroll
+        for (int j = 0; j < VN; ++j) {
+            const int i = j * 256 + (int)threadIdx.x;
+            if (i < n * (D / 8)) *reinterpret_cast<uint4*>(&tile[slot + i / (D / 8)][i % (D / 8) * 8]) = v[j];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < KN; ++j) {
+        const int i = j * 256 + (int)threadIdx.x;
+        if (i < n * TASKS) {
+            const int t = i / TASKS;
+            int fa, fb;
+            pair_task<INTERLEAVED>(i % TASKS, a.rd, fa, fb);
+            bf16x8 p = as_bf16x8(x[j]), q = as_bf16x8(y[j]);
+            turn_pairs<INTERLEAVED>(i % TASKS, a.rd, angles(t), p, q);
+            char* const dst = kt + (size_t)(slot + t) * D * EL;
+            if constexpr (FP8) {
+                *reinterpret_cast<uint2*>(dst + fa) = e4m3_from_bf16x8(p, it.k_inv);
+                *reinterpret_cast<uint2*>(dst + fb) = e4m3_from_bf16x8(q, it.k_inv);
+            } else {
+                st_global_16(dst + fa * 2, as_uint4(p));
+                st_global_16(dst + fb * 2, as_uint4(q));
+            }
+        }
+    }
+    const auto store_one = [&](int d, int place, bf16 value) RS_INLINE {
+        if constexpr (FP8) reinterpret_cast<uint8_t*>(vt)[d * 64 + place] = (uint8_t)(e4m3_pair(bf16_to_f32(value) * it.v_inv, 0.0f) & 0xffu);
+        else reinterpret_cast<bf16*>(vt)[d * 64 + place] = value;
     };
-    if (n <= APPEND_FEW && !it.zero_tail) {   // values, one by one
+    if (!turned) {   // values, one by one
         for (int i = threadIdx.x; i < n * D; i += 256) store_one(i % D, slot + i / D, v0[(size_t)(i / D) * a.ld_v + i % D]);
         return;
-    }
-    __shared__ __attribute__((aligned(16))) bf16 tile[64][D + 8];
-    for (int i = threadIdx.x; i < n * (D / 8); i += 256) {
-        const int t = i / (D / 8), ch = i % (D / 8);
-        *reinterpret_cast<uint4*>(&tile[slot + t][ch * 8]) = ld_global_16(v0 + (size_t)t * a.ld_v + ch * 8);
     }
     __syncthreads();
     for (int i = threadIdx.x; i < D * 8; i += 256) {   // feature i / 8, places 8 (i % 8) ..
