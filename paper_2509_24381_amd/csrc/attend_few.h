@@ -114,38 +114,53 @@ struct FewRows {
     __device__ __forceinline__ int head(int i) const { return kvh * g + (LIST ? i : i % g); }
 };
 
-// How a wavefront streams a tile: its keys, then its values (V^T), in PER units each of BYTES contiguous bytes.  16-byte chunks sit at places
+constexpr int FEW_UNIT = 4096;   // bytes of a unit (a tile's keys or values, if they are fewer)
+// How a wavefront streams a tile: its keys, then its values (V^T), in PER units each of BYTES bytes.  16-byte chunks sit at places
 // of their row that make the 8 lanes of a read, which are 8 keys or features of one chunk, meet different banks; a load instruction
 // fills 1 KB of LDS linearly by lane, each lane fetching the chunk that belongs in its place.
 template <int D, bool FP8>
 struct FewUnit {
     static constexpr int EL = FP8 ? 1 : 2;
     static constexpr int TILE = 64 * D * EL;                    // bytes of a tile's keys, or values
-    static constexpr int PER = TILE > 8192 ? TILE / 8192 : 1;
+    static constexpr int PER = TILE > FEW_UNIT ? TILE / FEW_UNIT : 1;
     static constexpr int BYTES = TILE / PER, LOADS = BYTES / 1024;
+    static constexpr int SUBS = 4 / PER;                        // sub-tiles of 16 keys in a K unit
     static constexpr int K_ROW = D * EL, K_CHUNKS = K_ROW / 16;   // a key's bytes, chunks
     static constexpr int K_READS = K_CHUNKS / 4;                // 16-byte reads of a lane per 16 keys
     static constexpr int V_ROW = 64 * EL;                       // a feature's bytes
     static constexpr int V_READS = V_ROW / 64;                  // 16-byte reads of a lane per 16 features
+    static_assert(SUBS >= 1, "a K unit is whole sub-tiles");
     // Key of MFMA row i of sub-tile t: the scores a lane ends up with - rows 4 c .. 4 c + 3 of every sub-tile - are the keys it multiplies
     // with values, consecutive ones: 8 of every 32, or with 8-bit values, which come 16 to a chunk, 16 of 64.
     RS_UNIT static int key_of(int t, int i) {
         return FP8 ? (i >> 2) * 16 + t * 4 + (i & 3) : (t >> 1) * 32 + (i >> 2) * 8 + (t & 1) * 4 + (i & 3);
     }
-    RS_UNIT static int k_swizzle(int key) {   // of a key's chunks: from its MFMA row
-        const int i = (key & 3) | ((FP8 ? key >> 4 : key >> 3) & 3) << 2;
+    // A K unit's rows in LDS are its keys in order, four groups of 4 SUBS neighbours (bfloat16 with SUBS = 4: two times four groups of 8).
+    // Row of MFMA row i of the unit's first sub-tile, rows from there to sub-tile t, and back: MFMA row of a row; key of a row of unit h.
+    static constexpr int GROUP = FP8 || SUBS < 4 ? 4 * SUBS : 8;
+    RS_UNIT static int row_of(int i) { return (i >> 2) * GROUP + (i & 3); }
+    RS_UNIT static constexpr int sub_step(int t) { return !FP8 && SUBS == 4 ? (t >> 1) * 32 + (t & 1) * 4 : t * 4; }
+    RS_UNIT static int mfma_row(int row) { return (row / GROUP & 3) * 4 + (row & 3); }
+    RS_UNIT static constexpr int key_of_row(int h, int row) {
+        if (SUBS == 4) return row;
+        if (FP8) return row / GROUP * 16 + h * GROUP + row % GROUP;
+        return SUBS == 2 ? h * 32 + row : (h >> 1) * 32 + row / 4 * 8 + (h & 1) * 4 + row % 4;
+    }
+    RS_UNIT static int k_swizzle(int row) {   // of a row's chunks: from its MFMA row
+        const int i = mfma_row(row);
         return K_CHUNKS == 16 ? i : K_CHUNKS == 8 ? i & 7 : (i >> 1) & 3;
     }
     RS_UNIT static int v_swizzle(int feature) { return V_ROW == 128 ? feature & 7 : (feature >> 1) & 3; }
-    RS_UNIT static uint32_t k_place(int key, int chunk) { return (uint32_t)(key * K_ROW + (chunk ^ k_swizzle(key)) * 16); }
+    RS_UNIT static uint32_t k_place(int row, int chunk) { return (uint32_t)(row * K_ROW + (chunk ^ k_swizzle(row)) * 16); }
     RS_UNIT static uint32_t v_place(int feature, int chunk) { return (uint32_t)(feature * V_ROW + (chunk ^ v_swizzle(feature)) * 16); }
-    // bytes from a lane's chunks of sub-tile 0 to those of sub-tile t (the swizzle is the MFMA row's: the same); a unit has 4 / PER sub-tiles
-    RS_UNIT static constexpr int k_step(int t) { return (FP8 ? t * 4 : (t >> 1) * 32 + (t & 1) * 4) * K_ROW; }
-    // where in the unit the chunk that belongs at place p (16 bytes each) is
-    RS_UNIT static uint32_t k_source(int p) { return k_place(p / K_CHUNKS, p % K_CHUNKS); }
-    RS_UNIT static uint32_t v_source(int p) { return v_place(p / (V_ROW / 16), p % (V_ROW / 16)); }
-    // load instructions after which the keys' sources repeat, as many keys further on (values': every one, a KB is 8 or 16 features)
-    static constexpr int K_PATTERNS = (FP8 ? 64 : 32) * K_ROW / 1024 < LOADS ? (FP8 ? 64 : 32) * K_ROW / 1024 : LOADS;
+    // Load instruction i fills rows K_LOAD i .. of the unit, keys that are neighbours: where in them a lane's chunk is, and where they are
+    // in the tile.  (Values: contiguous, and every instruction like the first: a KB is 8 or 16 features.)
+    static constexpr int K_LOAD = 1024 / K_ROW;
+    RS_UNIT static uint32_t k_source(int i, int lane) {
+        return (uint32_t)(lane / K_CHUNKS * K_ROW + (lane % K_CHUNKS ^ k_swizzle(i * K_LOAD + lane / K_CHUNKS)) * 16);
+    }
+    RS_UNIT static constexpr int k_start(int h, int i) { return key_of_row(h, i * K_LOAD) * K_ROW; }
+    RS_UNIT static uint32_t v_source(int lane) { return v_place(lane / (V_ROW / 16), lane % (V_ROW / 16)); }
 };
 
 // ONCE: nothing that is read is read again soon.
@@ -153,8 +168,10 @@ constexpr int FEW_ONCE = 2;   // cache policy (nt)
 template <int D, bool FP8, bool LIST, bool ONCE, bool INLINE>
 __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a, std::conditional_t<INLINE, InlineTable, NoTable> tab) {
     typedef FewUnit<D, FP8> U;
-    constexpr int KS = D / 32, DT = D / 16, NT = 4 / U::PER, DTU = DT / U::PER;   // sub-tiles of a K unit, feature blocks of a V unit
-    __shared__ __attribute__((aligned(16))) char lds[FEW_WAVES * 2 * U::BYTES];   // each wavefront's keys and values, in the end its sums
+    constexpr int KS = D / 32, DT = D / 16, NT = U::SUBS, DTU = DT / U::PER;   // sub-tiles of a K unit, feature blocks of a V unit
+    // each wavefront's keys and values, in the end all their sums
+    constexpr int LDS_BYTES = FEW_WAVES * (2 * U::BYTES > 16 * (D + 4) * 4 ? 2 * U::BYTES : 16 * (D + 4) * 4);
+    __shared__ __attribute__((aligned(16))) char lds[LDS_BYTES];
     __shared__ float m_sh[FEW_WAVES][16], l_sh[FEW_WAVES][16];
     const uint32_t* const table = table_of<INLINE>(tab, a.table);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -236,9 +253,10 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
     typedef __attribute__((address_space(3))) void* lds_ptr;
     char* const mine = lds + wave * 2 * U::BYTES;
     const uint64_t k_head = rq.k + (uint64_t)rows.kvh * rq.head_bytes, v_head = rq.v + (uint64_t)rows.kvh * rq.head_bytes;
-    uint32_t k_src[8];   // where a lane's 16 bytes of a load instruction come from (U::K_PATTERNS of them; values: one)
+    uint32_t k_src[8];   // where a lane's 16 bytes of a load instruction come from
+    static_assert(U::LOADS <= 8, "k_src");
 #pragma unroll
-    for (int i = 0; i < U::K_PATTERNS; ++i) k_src[i] = U::k_source(i * 64 + lane);
+    for (int i = 0; i < U::LOADS; ++i) k_src[i] = U::k_source(i, lane);
     const uint32_t v_src = U::v_source(lane);
     // unit h of tile j: 0 .. PER - 1 its keys, then its values; unit h goes to place h & 1
     const auto fetch = [&](int j, int h) RS_INLINE {
@@ -248,8 +266,8 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
         char* const to = mine + (h & 1) * U::BYTES;
 #pragma unroll
         for (int i = 0; i < U::LOADS; ++i) {
-            const uint32_t from = keys ? k_src[i % U::K_PATTERNS] : v_src;   // (named: template-dependent arguments of the builtin break the host-side stub)
-            const int further = h % U::PER * U::BYTES + (keys ? i / U::K_PATTERNS * U::K_PATTERNS : i) * 1024;
+            const uint32_t from = keys ? k_src[i] : v_src;   // (named: template-dependent arguments of the builtin break the host-side stub)
+            const int further = keys ? U::k_start(h, i) : h % U::PER * U::BYTES + i * 1024;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)(uintptr_t)(uint32_t)(uintptr_t)(to + i * 1024), 16, from, further, 0, ONCE ? FEW_ONCE : 0);
         }
     };
@@ -266,7 +284,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
     };
     uint32_t k_at[4], v_at[2];   // a lane's fragments: sub-tile 0, features 0 .. 15
 #pragma unroll
-    for (int i = 0; i < U::K_READS; ++i) k_at[i] = U::k_place(U::key_of(0, r), i * 4 + c);
+    for (int i = 0; i < U::K_READS; ++i) k_at[i] = U::k_place(U::row_of(r), i * 4 + c);
 #pragma unroll
     for (int i = 0; i < U::V_READS; ++i) v_at[i] = U::v_place(r, i * 4 + c);
 
@@ -299,7 +317,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int i = 0; i < U::K_READS; ++i)
-                    kf[t * U::K_READS + i] = *reinterpret_cast<const uint4*>(mine + (h & 1) * U::BYTES + k_at[i] + U::k_step(t));
+                    kf[t * U::K_READS + i] = *reinterpret_cast<const uint4*>(mine + (h & 1) * U::BYTES + k_at[i] + U::sub_step(t) * U::K_ROW);
             reads_done();
             refill(hc);
 #pragma unroll
@@ -376,8 +394,8 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
         block = __builtin_amdgcn_readlane(number, (j + 1) & 63);
     }
 
-    static_assert(16 * (D + 4) * 4 <= 2 * U::BYTES, "a wavefront's sums fit where its keys and values were");
-    const auto sums_of = [&](int w, int row) RS_INLINE { return reinterpret_cast<float*>(lds + w * 2 * U::BYTES) + row * (D + 4); };
+    constexpr int SUMS = 16 * (D + 4) * 4;   // bytes of a wavefront's sums
+    const auto sums_of = [&](int w, int row) RS_INLINE { return reinterpret_cast<float*>(lds + w * SUMS) + row * (D + 4); };
     // ---- the wavefronts of the same rows meet: each brings its sums to the largest reference among them
     l += __shfl_xor(l, 16, WAVE);
     l += __shfl_xor(l, 32, WAVE);
