@@ -84,8 +84,9 @@ rs_status rs_kv_append(rs_ctx* ctx, const rs_rotary* rotary, int layer, rs_kv* c
  * lens[i] <= rs_kv_len (RS_EINVAL).  scale: 0 stands for 1 / sqrt(head_dim), else positive and finite.  out may be q.
  * Scores, softmax statistics and sums are fp32, the softmax's weights enter the second product as bfloat16, the output is
  * rounded once.  What a query does not see does not reach it, infinities and NaN included.
- * Requests of few rows (rows * Hq / Hkv <= 64) read 8-bit caches directly, as code * scale; longer ones expand what they see
- * into the workspace first, as rs_prefill_* do (the value is then rounded to bfloat16).
+ * Requests of few rows (rows * Hq / Hkv <= 64, or more where little is cached) read 8-bit caches directly, as code * scale; longer ones
+ * expand what they see into the workspace first, as rs_prefill_* do (the value is then rounded to bfloat16).
+ * RS_ATTEND_FEW=n, a TEST-ONLY environment variable read in rs_ctx_create, replaces the size up to which "more rows" are few (0: never).
  *   workspace   256-byte aligned, rs_attend_workspace_bytes:
  *     max_rows, max_requests   of a call
  *     max_visible_fp8          8-bit caches in calls with longer requests: the sum of their cached tokens, else 0

@@ -26,30 +26,32 @@
 #include "exact_row.h"
 #include "kv_fp8.h"
 
-// Descriptors of a call: in the kernel arguments where they fit, else copied to the workspace ahead of the kernel (read in place they
-// would cross the host link once per workgroup).
-constexpr int TABLE_WORDS = 880;
+// Descriptors of a call: in the kernel arguments where they fit, else copied to the workspace ahead of the kernel.  Page numbers that do not fit
+// beside them are read where the host left them: a wavefront does it once per 64 tiles.  (All of it read in place: three such reads, one after
+// the other, at the start of every workgroup, as long as the copy.)
+constexpr int TABLE_WORDS = 928;
 struct InlineTable { uint32_t w[TABLE_WORDS]; };
 struct NoTable {};
 
 constexpr int32_t CONTIGUOUS = INT32_MIN;
 
-// One request, 64 bytes.  The tile of block b (V: v) of KV head h:  k + h * head_bytes + index * block_bytes, index = b in a contiguous
-// cache, the block's page in a paged one.
+// One request, 48 bytes.  The keys' tile of block b of KV head h:  k + (h head_tiles + index) tile in a contiguous cache, index = b, and
+// k + (2 Hkv index + h) tile in a paged one, index = the block's page; values Hkv head_tiles tiles further on (a page holds its KV heads'
+// keys, then their values: head_tiles = 1).
 struct FewReq {
-    uint64_t k, v;
-    uint64_t head_bytes;
-    uint32_t block_bytes;
-    int32_t pages;         // number of block b: word pages + b of the table; CONTIGUOUS: b itself
+    uint64_t k;
+    int32_t head_tiles;
+    int32_t pages;         // its first page number's place among the page numbers; CONTIGUOUS: the cache is
     int32_t row0, T, P;    // first row, rows, position of the first row
     int32_t parts;         // parts of the key range
     int32_t slot0;         // of its first part
     float k_scale, v_scale;
     int32_t pad_;
 };
-static_assert(sizeof(FewReq) == 64, "sixteen words");
+constexpr int REQ_WORDS = 12;
+static_assert(sizeof(FewReq) == 4 * REQ_WORDS, "REQ_WORDS");
 
-// Table: every request's first item, and its first unit (what few_merge_kernel joins), each padded to 16 bytes; requests; page numbers.
+// Table: every request's first item, and its first unit (what few_merge_kernel joins), each padded to 16 bytes; requests.
 __host__ __device__ inline int table_units_at(int n_req) { return (n_req + 3) & ~3; }
 __host__ __device__ inline int table_reqs_at(int n_req) { return 2 * table_units_at(n_req); }
 
@@ -82,6 +84,7 @@ RS_DEVICE bf16x8 bf16x8_of_codes(uint32_t lo, uint32_t hi) {
 }
 struct FewArgs {
     const uint32_t* table;   // device table (not INLINE)
+    const uint32_t* pages;   // page numbers; null: behind the table's requests
     int n_req, hkv, g;
     const bf16* q;
     long ld_q;
@@ -106,12 +109,19 @@ struct FewSlot {   // of a part and 16 rows: [16][D] sums, then references, then
     static constexpr size_t FLOATS = (size_t)16 * (D + 2);
 };
 
+constexpr int FEW_GROUP = 64;          // stacked rows of an item
 // An item's rows, and where they are in q and out.
 template <bool LIST>
 struct FewRows {
-    int row0, P, kvh, g, tok0, rows;   // (LIST: the g heads of one token)
-    __device__ __forceinline__ int token(int i) const { return LIST ? tok0 : i / g; }
-    __device__ __forceinline__ int head(int i) const { return kvh * g + (LIST ? i : i % g); }
+    int row0, P, kvh, g, first, tok0, rows;   // first: of the request's stacked rows; tok0: its token.  (LIST: the g heads of one token)
+    __device__ __forceinline__ int token(int i) const { return LIST ? tok0 : (first + i) / g; }
+    __device__ __forceinline__ int head(int i) const { return kvh * g + (LIST ? i : (first + i) % g); }
+    // Takes the rows of group `group` of a request's `all`.
+    __device__ __forceinline__ void take(int group, int all) {
+        first = group * FEW_GROUP;
+        rows = min(FEW_GROUP, all - first);
+        tok0 = first / g;
+    }
 };
 
 constexpr int FEW_UNIT = 4096;   // bytes of a unit (a tile's keys or values, if they are fewer)
@@ -198,6 +208,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
         unit = part = parts = 0;
     }
     const FewReq rq = reinterpret_cast<const FewReq*>(table + table_reqs_at(a.n_req))[req];
+    const uint32_t* const pages = a.pages ? a.pages : table + table_reqs_at(a.n_req) + REQ_WORDS * a.n_req;
     rows.row0 = rq.row0;
     rows.P = rq.P;
     if constexpr (LIST) {
@@ -205,23 +216,26 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
         list = a.chosen + (size_t)unit * a.n_blocks;
         n = min(a.n_blocks, (rq.P + rows.tok0) / 64 + 1);   // (the list ends there)
     } else {
-        const int id = (int)(blockIdx.x - table[req]);
+        int id = (int)(blockIdx.x - table[req]);
         parts = rq.parts;
-        unit = rows.kvh = id % a.hkv;
-        part = id / a.hkv;
-        rows.tok0 = 0;
-        rows.rows = rq.T * a.g;
-        n = (rq.P + rq.T - 1) / 64 + 1;
+        rows.kvh = id % a.hkv;
+        id /= a.hkv;
+        part = id % parts;
+        rows.take(id / parts, rq.T * a.g);
+        unit = id / parts * a.hkv + rows.kvh;
+        n = (rq.P + rows.token(rows.rows - 1)) / 64 + 1;
     }
     const int kb0 = (int)((long)n * part / parts), kb1 = (int)((long)n * (part + 1) / parts);
     const int rbn = few_row_blocks(rows.rows), rb = wave & (rbn - 1), step = FEW_WAVES / rbn;
-    const auto tile_at = [&](int i, global_bytes& kt, global_bytes& vt, int& block) RS_INLINE {
+    const int slot_blocks = LIST ? rbn : few_row_blocks(min(rq.T * a.g, FEW_GROUP));   // of a part (the last group may have fewer)
+    const uint64_t k_head = rq.k + (uint64_t)rows.kvh * (uint32_t)rq.head_tiles * U::TILE;
+    const uint64_t v_head = k_head + (uint64_t)a.hkv * (uint32_t)rq.head_tiles * U::TILE;
+    const auto tile_at = [&](int i, global_bytes& kt, global_bytes& vt, int& block) RS_INLINE {   // (exact_row's)
         block = i;
         if constexpr (LIST) block = list[i];
-        const uint64_t index = rq.pages == CONTIGUOUS ? (uint32_t)block : table[rq.pages + block];
-        const uint64_t off = (uint64_t)rows.kvh * rq.head_bytes + index * rq.block_bytes;
-        kt = (global_bytes)(rq.k + off);
-        vt = (global_bytes)(rq.v + off);
+        const uint64_t at = rq.pages == CONTIGUOUS ? (uint64_t)(uint32_t)block : (uint64_t)pages[rq.pages + block] * (uint32_t)(2 * a.hkv);
+        kt = (global_bytes)(k_head + at * U::TILE);
+        vt = (global_bytes)(v_head + at * U::TILE);
     };
 
     // ---- queries
@@ -248,11 +262,11 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
     const auto look_up = [&](int j0) RS_INLINE {   // of tiles j0 .. j0 + 63
         const int i = min(first + (j0 + lane) * step, kb1 - 1);
         number = LIST ? list[i] : i;
-        place = rq.pages == CONTIGUOUS ? number : (int)table[rq.pages + number];
+        place = rq.pages == CONTIGUOUS ? number : (int)pages[rq.pages + number];
     };
     typedef __attribute__((address_space(3))) void* lds_ptr;
     char* const mine = lds + wave * 2 * U::BYTES;
-    const uint64_t k_head = rq.k + (uint64_t)rows.kvh * rq.head_bytes, v_head = rq.v + (uint64_t)rows.kvh * rq.head_bytes;
+    const uint32_t place_bytes = (rq.pages == CONTIGUOUS ? 1u : 2u * (uint32_t)a.hkv) * U::TILE;
     uint32_t k_src[8];   // where a lane's 16 bytes of a load instruction come from
     static_assert(U::LOADS <= 8, "k_src");
 #pragma unroll
@@ -262,7 +276,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
     const auto fetch = [&](int j, int h) RS_INLINE {
         const bool keys = h < U::PER;
         const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-            (void*)((keys ? k_head : v_head) + (uint64_t)(uint32_t)__builtin_amdgcn_readlane(place, j & 63) * rq.block_bytes), 0, U::TILE, 0x00020000);
+            (void*)((keys ? k_head : v_head) + (uint64_t)(uint32_t)__builtin_amdgcn_readlane(place, j & 63) * place_bytes), 0, U::TILE, 0x00020000);
         char* const to = mine + (h & 1) * U::BYTES;
 #pragma unroll
         for (int i = 0; i < U::LOADS; ++i) {
@@ -435,7 +449,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
         const bool live = i < rows.rows;
         const int ic = min(i, rows.rows - 1);
         bf16* const op = a.out + (size_t)(rq.row0 + rows.token(ic)) * a.ld_out + rows.head(ic) * D;
-        float* const slot = a.slots + (size_t)(rq.slot0 + (unit * parts + part) * rbn + b) * FewSlot<D>::FLOATS;
+        float* const slot = a.slots + (size_t)(rq.slot0 + (unit * parts + part) * slot_blocks + b) * FewSlot<D>::FLOATS;
         const unsigned long long any = __builtin_amdgcn_ballot_w64(bad && live);
         const bool again = ((any >> (lane & 48)) & 0xffffu) != 0;   // (a row's sixteen threads are neighbours)
         if (!again && parts > 1) {
@@ -509,17 +523,19 @@ __global__ __launch_bounds__(256) void few_merge_kernel(FewArgs a, std::conditio
         rows.tok0 -= rq.row0;
         rows.rows = a.g;
     } else {
-        rows.tok0 = 0;
-        rows.rows = rq.T * a.g;
-        const int id = (int)(blockIdx.x - table[table_units_at(a.n_req) + req]);
-        unit = rows.kvh = id % a.hkv;
-        b = id / a.hkv;
+        int id = (int)(blockIdx.x - table[table_units_at(a.n_req) + req]);   // (four row blocks per KV head and group, if there are)
+        const int most = few_row_blocks(min(rq.T * a.g, FEW_GROUP));
+        rows.kvh = id % a.hkv;
+        id /= a.hkv;
+        b = id % most;
+        rows.take(id / most, rq.T * a.g);
+        unit = id / most * a.hkv + rows.kvh;
     }
-    const int rbn = few_row_blocks(rows.rows);
     if (b * 16 >= rows.rows) return;
     const int group = threadIdx.x >> 6, row = (threadIdx.x & 63) >> 2, f0 = blockIdx.y * 32 + (threadIdx.x & 3) * 8, i = b * 16 + row;
-    const float* const base = a.slots + (size_t)(rq.slot0 + unit * parts * rbn + b) * FewSlot<D>::FLOATS;
-    const size_t next = (size_t)rbn * FewSlot<D>::FLOATS;
+    const int slot_blocks = few_row_blocks(LIST ? a.g : min(rq.T * a.g, FEW_GROUP));
+    const float* const base = a.slots + (size_t)(rq.slot0 + unit * parts * slot_blocks + b) * FewSlot<D>::FLOATS;
+    const size_t next = (size_t)slot_blocks * FewSlot<D>::FLOATS;
     // four parts at a time, all their loads in flight together, on to a running reference M
     float M = -INFINITY, L = 0.0f, o[8] = {};
     for (int p0 = group; p0 < parts; p0 += 16) {
@@ -576,7 +592,7 @@ __global__ __launch_bounds__(256) void few_merge_kernel(FewArgs a, std::conditio
         bf16x8 h;
 #pragma unroll
         for (int e = 0; e < 8; ++e) h[e] = f32_to_bf16(((red[0][t][e] + red[1][t][e]) + (red[2][t][e] + red[3][t][e])) * inv);
-        *reinterpret_cast<bf16x8*>(a.out + (size_t)(rq.row0 + rows.tok0 + (LIST ? 0 : i / a.g)) * a.ld_out + rows.head(i) * D + f0) = h;
+        *reinterpret_cast<bf16x8*>(a.out + (size_t)(rq.row0 + rows.token(i)) * a.ld_out + rows.head(i) * D + f0) = h;
     }
 }
 

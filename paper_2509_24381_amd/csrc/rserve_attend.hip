@@ -27,7 +27,14 @@ struct rs_rotary {
 
 namespace {
 
-constexpr int FEW_ROWS = 64;       // stacked rows of a request up to which it goes to attend_few_kernel
+// Requests of up to 64 stacked rows go to attend_few_kernel, and so do the others of a call if they have little to read: their row groups times
+// KV heads times tiles, all together, up to these.  The chunk kernel needs its descriptors in the workspace first (a launch), a merge more often,
+// and 8-bit caches expanded.  us a pass, chunk kernel / attend_few_kernel, 28 query heads, 4 KV heads: 64 tokens on 2000 (896 of them)
+// 20.4 / 17.5, 96 on 2000 (1408) 22.5 / 23.5, 32 on 8000 (2000) 23.1 / 26.3, 12 on 30000 (3752) 37.9 / 43.4; 64 heads, 8 KV heads: 32 on 2000
+// (1024) 20.2 / 19.8, 48 (1536) 22.3 / 24.1; 8 bits: 128 on 2000 (1792) 31.3 / 22.8, 128 on 8000 (7000) 39.0 / 38.8, 48 on 30000 (11256)
+// 58.3 / 58.8.
+constexpr int FEW_ROWS = FEW_GROUP;
+constexpr long FEW_TILES = 1100, FEW_TILES_FP8 = 8000;
 // Caches that one call reads once are loaded with the streaming hint, unless they are so small that the L2s may still have them from a call
 // before.  us with / without it, behind a fill of 1 GB: 8 MB 14.6 / 15.6, 35 MB 19.6 / 26.6, 141 MB 38.3 / 69.5; call after call on the
 // same caches: 4 MB 15.7 / 14.6, 8 MB 20.2 / 20.4, 141 MB 53.3 / 54.5.
@@ -246,31 +253,31 @@ void plan_few(std::vector<FewRequest>& reqs, int places, size_t slots) {
     for (FewRequest& r : reqs) r.parts = std::min((r.tiles + best_len - 1) / best_len, FEW_MAX_PARTS);
 }
 
-// The table of `reqs` at `w` (`words` of room, checked by the caller).  LIST: items are rows.
+// The table of `reqs` at `w` (`words` of room, checked by the caller), their page numbers at `pages`.  LIST: items are rows.
 struct FewTable {
     uint32_t items = 0, units = 0;
     bool any_split = false;
 };
-FewTable write_few_table(const rs_ctx* ctx, int layer, rs_kv* const* kvs, const std::vector<FewRequest>& reqs, bool list, uint32_t* w) {
+FewTable write_few_table(const rs_ctx* ctx, int layer, rs_kv* const* kvs, const std::vector<FewRequest>& reqs, bool list, uint32_t* w, uint32_t* pages) {
     const int n = (int)reqs.size();
     FewTable t;
-    int page_at = table_reqs_at(n) + 16 * n, slot = 0;
+    int page_at = 0, slot = 0;
     for (int j = 0; j < n; ++j) {
         const FewRequest& r = reqs[j];
         const rs_kv* kv = kvs[r.kv];
-        const TilePlaces p = places_of(kv, layer);
         FewReq q{};
-        q.k = p.k; q.v = p.v; q.head_bytes = p.head_bytes; q.block_bytes = p.block_bytes;
+        q.k = places_of(kv, layer).k;
+        q.head_tiles = kv->paged() ? 1 : kv->cap / 64;
         q.pages = CONTIGUOUS;
         if (kv->paged()) {
             q.pages = page_at;
-            for (int b = 0; b < r.tiles; ++b) w[page_at++] = (uint32_t)kv->pages[layer][b];
+            for (int b = 0; b < r.tiles; ++b) pages[page_at++] = (uint32_t)kv->pages[layer][b];
         }
         q.row0 = r.row0; q.T = r.T; q.P = kv->len[layer] - r.T;
         q.parts = r.parts;
         q.slot0 = list ? 0 : slot;
         q.k_scale = kv->k_scale; q.v_scale = kv->v_scale;
-        memcpy(&w[table_reqs_at(n) + 16 * j], &q, sizeof(q));
+        memcpy(&w[table_reqs_at(n) + REQ_WORDS * j], &q, sizeof(q));
         w[j] = list ? (uint32_t)r.row0 : t.items;
         w[table_units_at(n) + j] = t.units;
         t.items += (uint32_t)(r.units * r.parts);
@@ -282,10 +289,11 @@ FewTable write_few_table(const rs_ctx* ctx, int layer, rs_kv* const* kvs, const 
     }
     return t;
 }
-size_t few_table_words(const rs_ctx*, rs_kv* const* kvs, const std::vector<FewRequest>& reqs) {
-    size_t words = table_reqs_at((int)reqs.size()) + 16 * reqs.size();
-    for (const FewRequest& r : reqs) words += kvs[r.kv]->paged() ? r.tiles : 0;
-    return words;
+size_t few_table_words(const std::vector<FewRequest>& reqs) { return table_reqs_at((int)reqs.size()) + REQ_WORDS * reqs.size(); }
+size_t few_table_pages(rs_kv* const* kvs, const std::vector<FewRequest>& reqs) {
+    size_t n = 0;
+    for (const FewRequest& r : reqs) n += kvs[r.kv]->paged() ? r.tiles : 0;
+    return n;
 }
 
 template <bool LIST>
@@ -588,13 +596,18 @@ rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, 
     const rs_layer_cfg& f = ctx->cfg;
     const AttendLayout L = attend_layout(f, (int)rows, R, 0);
     const bool fp8 = kvs[0]->fp8;
+    const auto stacked_rows = [&](int i) { return (long)lens[i] * ctx->group; };
+    const auto row_groups = [&](int i) { return (stacked_rows(i) + FEW_GROUP - 1) / FEW_GROUP; };
     size_t expansion = 0;
-    bool chunks = false;
+    long tiles = 0;   // of the requests with more rows
     for (int i = 0; i < R; ++i)
-        if ((long)lens[i] * ctx->group > FEW_ROWS) {
-            chunks = true;
+        if (stacked_rows(i) > FEW_ROWS) {
+            tiles += row_groups(i) * f.n_kv_heads * ((kvs[i]->len[layer] + 63) / 64);
             if (fp8) expansion += expansion_bytes(ctx, kvs[i]->len[layer]);
         }
+    const bool chunks = tiles > (ctx->few_tiles >= 0 ? ctx->few_tiles : fp8 ? FEW_TILES_FP8 : FEW_TILES);
+    const auto is_few = [&](int i) { return lens[i] > 0 && (!chunks || stacked_rows(i) <= FEW_ROWS); };
+    if (!chunks) expansion = 0;
     if ((s = check_workspace(workspace, workspace_bytes, L.total + expansion)) != RS_OK) return s;
     if (chunks && (ld_q > 0x7fffffff || ld_out > 0x7fffffff)) return fail(RS_EINVAL, "ld beyond 2^31");
     if ((s = check_device(ctx)) != RS_OK) return s;
@@ -607,38 +620,46 @@ rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, 
     std::vector<FewRequest> few;
     int row = 0;
     for (int i = 0; i < R; ++i) {
-        const long stacked = (long)lens[i] * ctx->group;
-        if (lens[i] > 0 && stacked <= FEW_ROWS)
-            few.push_back(FewRequest{i, row, lens[i], f.n_kv_heads, (kvs[i]->len[layer] + 63) / 64, few_row_blocks((int)stacked), 1});
+        if (is_few(i))
+            few.push_back(FewRequest{i, row, lens[i], (int)row_groups(i) * f.n_kv_heads, (kvs[i]->len[layer] + 63) / 64,
+                                     few_row_blocks((int)std::min<long>(stacked_rows(i), FEW_GROUP)), 1});
         row += lens[i];
     }
     FewArgs a{};
     FewTable ft;
     InlineTable tab;
-    bool inline_table = false;
+    enum { NOTHING, PAGES, ALL } few_staged = NOTHING;   // of the table (see TABLE_WORDS)
     size_t few_words = 0, few_bytes = 0;   // few_bytes: of the keys and values they read
+    bool once = true;                      // nobody reads them twice
     if (!few.empty()) {
-        for (const FewRequest& r : few) few_bytes += (size_t)r.tiles * 128 * ctx->kv_dim * (fp8 ? 1 : 2);
-
+        for (const FewRequest& r : few) {
+            few_bytes += (size_t)r.tiles * 128 * ctx->kv_dim * (fp8 ? 1 : 2);
+            once &= r.units == f.n_kv_heads;
+        }
         plan_few(few, FEW_PLACES * ctx->n_cu, SLOT_ROWS / 16);
         a.n_req = (int)few.size();
         a.hkv = f.n_kv_heads; a.g = ctx->group;
         a.q = (const bf16*)q; a.ld_q = ld_q; a.out = (bf16*)out; a.ld_out = ld_out;
         a.scale_log2e = scale_log2e;
         a.slots = reinterpret_cast<float*>(ws + L.slots_at);
-        few_words = few_table_words(ctx, kvs, few);
-        inline_table = few_words <= TABLE_WORDS;
-        if (inline_table) ft = write_few_table(ctx, layer, kvs, few, false, tab.w);
+        few_words = few_table_words(few);
+        const size_t pages = few_table_pages(kvs, few);
+        few_staged = few_words + pages <= TABLE_WORDS ? NOTHING : few_words <= TABLE_WORDS ? PAGES : ALL;
+        if (few_staged == NOTHING) ft = write_few_table(ctx, layer, kvs, few, false, tab.w, tab.w + few_words);
     }
-    const bool staged = chunks || (!few.empty() && !inline_table);
+    const bool staged = chunks || few_staged != NOTHING;
     int slot = 0;
     if (staged && (s = ring_acquire(ctx, st, &slot)) != RS_OK) return s;
     char* const stage = staged ? ctx->pinned[slot] : nullptr;
     size_t staged_bytes = 0;
-    if (!few.empty() && !inline_table) {
-        ft = write_few_table(ctx, layer, kvs, few, false, reinterpret_cast<uint32_t*>(stage));
+    if (few_staged == ALL) {
+        ft = write_few_table(ctx, layer, kvs, few, false, reinterpret_cast<uint32_t*>(stage), reinterpret_cast<uint32_t*>(stage) + few_words);
         a.table = reinterpret_cast<const uint32_t*>(ws);
-        staged_bytes = align_up(few_words * 4, 16);
+        staged_bytes = align_up((few_words + few_table_pages(kvs, few)) * 4, 16);
+    } else if (few_staged == PAGES) {
+        ft = write_few_table(ctx, layer, kvs, few, false, tab.w, reinterpret_cast<uint32_t*>(stage));
+        a.pages = reinterpret_cast<const uint32_t*>(ctx->pinned_dev[slot]);
+        staged_bytes = align_up(few_table_pages(kvs, few) * 4, 16);
     }
     // ---- chunks
     std::vector<ReqDesc> reqs;
@@ -654,7 +675,7 @@ rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, 
         size_t expand_at = L.total;
         row = 0;
         for (int i = 0; i < R; row += lens[i], ++i) {
-            if ((long)lens[i] * ctx->group <= FEW_ROWS) continue;
+            if (stacked_rows(i) <= FEW_ROWS) continue;
             const rs_kv* kv = kvs[i];
             const int len = kv->len[layer];
             ReqDesc d = kv->view(layer, d_pagetab + pagetab.size());
@@ -695,16 +716,17 @@ rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, 
         memcpy(stage + at_mitems, plan.merges.data(), sizeof(AttnMergeItem) * plan.merges.size());
         memcpy(stage + at_fp8, fp8s.data(), sizeof(Fp8CacheDesc) * fp8s.size());
     }
-    if (staged) {
+    if (chunks || few_staged == ALL) {
         const int chunks16 = (int)(staged_bytes / 16);
         hipLaunchKernelGGL(copy_table_kernel, dim3((chunks16 + 255) / 256), dim3(256), 0, st, reinterpret_cast<const uint4*>(ctx->pinned_dev[slot]),
                            reinterpret_cast<uint4*>(ws), chunks16);
         RS_HIP(hipGetLastError());
-        if ((s = ring_commit(ctx, st)) != RS_OK) return s;
+        if (a.pages) a.pages = reinterpret_cast<const uint32_t*>(ws);   // (copied too)
     }
     if (!few.empty() &&
-        (s = launch_few<false>(ctx, fp8, few_bytes >= FEW_ONCE_BYTES, a, ft.items, ft.units, ft.any_split, inline_table ? &tab : nullptr, st)) != RS_OK)
+        (s = launch_few<false>(ctx, fp8, once && few_bytes >= FEW_ONCE_BYTES, a, ft.items, ft.units, ft.any_split, few_staged == ALL ? nullptr : &tab, st)) != RS_OK)
         return s;
+    if (staged && (s = ring_commit(ctx, st)) != RS_OK) return s;
     if (!chunks) return RS_OK;
     const ReqDesc* const d_reqs = reinterpret_cast<const ReqDesc*>(ws + at_reqs);
     const AttnItem* const d_items = reinterpret_cast<const AttnItem*>(ws + at_items);
@@ -768,7 +790,7 @@ rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int*
     if (s != RS_OK) return s;
     if (n_blocks < 1 || n_blocks > 1024 || n_first < 0 || n_last < 1)
         return fail(RS_EINVAL, "n_blocks = %d must be 1 .. 1024, n_first = %d at least 0, n_last = %d at least 1", n_blocks, n_first, n_last);
-    if (ctx->group > FEW_ROWS) return fail(RS_EINVAL, "%d query heads per KV head: more than %d", ctx->group, FEW_ROWS);
+    if (ctx->group > FEW_GROUP) return fail(RS_EINVAL, "%d query heads per KV head: more than %d", ctx->group, FEW_GROUP);
     for (int i = 0; i < R; ++i)
         if ((s = check_bounds(kvs[i], layer, i)) != RS_OK) return s;
     if (rows == 0) return RS_OK;
@@ -819,8 +841,9 @@ rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int*
     parts = std::max(1, std::min(parts, FEW_MAX_PARTS));
     int slot = 0;
     if ((s = ring_acquire(ctx, st, &slot)) != RS_OK) return s;
-    write_few_table(ctx, layer, kvs, reqs, true, reinterpret_cast<uint32_t*>(ctx->pinned[slot]));
-    const int copy_chunks = (int)(align_up(few_table_words(ctx, kvs, reqs) * 4, 16) / 16);
+    uint32_t* const table = reinterpret_cast<uint32_t*>(ctx->pinned[slot]);
+    write_few_table(ctx, layer, kvs, reqs, true, table, table + few_table_words(reqs));
+    const int copy_chunks = (int)(align_up((few_table_words(reqs) + few_table_pages(kvs, reqs)) * 4, 16) / 16);
     int* const list = chosen ? chosen : reinterpret_cast<int*>(ws + L.chosen_at);
 
     SelectArgs sa{};
