@@ -17,13 +17,14 @@
 // changes with it) and become bfloat16, exactly, in registers; their scales go into the softmax's scale and the output.
 //
 // Work item = (request, KV head, part of the key range), with up to 64 stacked rows.  A wavefront has 16 of them: with up to 16 rows the four
-// wavefronts of a workgroup take the item's tiles in turn, with up to 32 two pairs do, with more each takes every tile (the others'
+// wavefronts of a workgroup share the item's tiles, with up to 32 two pairs do, with more each takes every tile (the others'
 // loads of it hit in the caches; a wavefront with more rows of its own would have no registers for loads in flight).  They meet in LDS
 // once; parts leave unnormalised sums, references and row sums in slots that few_merge_kernel joins.
 #pragma once
 #include "attention.h"
 #include "common.h"
 #include "exact_row.h"
+#include "lanes.h"
 #include "kv_fp8.h"
 
 // Descriptors of a call: in the kernel arguments where they fit, else copied to the workspace ahead of the kernel.  Page numbers that do not fit
@@ -225,8 +226,9 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
         unit = id / parts * a.hkv + rows.kvh;
         n = (rq.P + rows.token(rows.rows - 1)) / 64 + 1;
     }
-    const int kb0 = (int)((long)n * part / parts), kb1 = (int)((long)n * (part + 1) / parts);
-    const int rbn = few_row_blocks(rows.rows), rb = wave & (rbn - 1), step = FEW_WAVES / rbn;
+    // (a part, and a wavefront's share of it: the quotient, one more for as many of the first as the remainder)
+    const int kb0 = n / parts * part + min(part, n % parts), held = n / parts + (part < n % parts);
+    const int rbn = few_row_blocks(rows.rows), rb = wave & (rbn - 1), sharers = FEW_WAVES / rbn, share = wave / rbn;
     const int slot_blocks = LIST ? rbn : few_row_blocks(min(rq.T * a.g, FEW_GROUP));   // of a part (the last group may have fewer)
     const uint64_t k_head = rq.k + (uint64_t)rows.kvh * (uint32_t)rq.head_tiles * U::TILE;
     const uint64_t v_head = k_head + (uint64_t)a.hkv * (uint32_t)rq.head_tiles * U::TILE;
@@ -256,11 +258,13 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
     float m = -INFINITY, l = 0.0f;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) acc[dt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    // ---- this wavefront's tiles kb0 + wave / rbn, + step, ...; their places (page or block) in a register, a lane each, 64 at a time
-    const int first = kb0 + wave / rbn, tiles = rb * 16 < rows.rows && first < kb1 ? (kb1 - first + step - 1) / step : 0;
+    // ---- this wavefront's share of the tiles; their places (page or block) in a register, a lane each, 64 at a time.  (Neighbours, so that page
+    // numbers read across the host link are few lines.)
+    const int first = kb0 + held / sharers * share + min(share, held % sharers), own = held / sharers + (share < held % sharers);
+    const int tiles = rb * 16 < rows.rows ? own : 0, last = max(first + own - 1, 0);
     int place = 0, number = 0;
     const auto look_up = [&](int j0) RS_INLINE {   // of tiles j0 .. j0 + 63
-        const int i = min(first + (j0 + lane) * step, kb1 - 1);
+        const int i = min(first + j0 + lane, last);
         number = LIST ? list[i] : i;
         place = rq.pages == CONTIGUOUS ? number : (int)pages[rq.pages + number];
     };
@@ -360,8 +364,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[t][e]);
-        mx = fmaxf(mx, __shfl_xor(mx, 16, WAVE));
-        mx = fmaxf(mx, __shfl_xor(mx, 32, WAVE)) * sc;
+        mx = of_quarters(mx, larger_of()) * sc;
         const bool move = mx > m + FEW_HEADROOM;   // (at first m is minus infinity)
         if (__builtin_amdgcn_ballot_w64(move)) {
             const float m_new = move ? mx : m;
@@ -411,8 +414,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
     constexpr int SUMS = 16 * (D + 4) * 4;   // bytes of a wavefront's sums
     const auto sums_of = [&](int w, int row) RS_INLINE { return reinterpret_cast<float*>(lds + w * SUMS) + row * (D + 4); };
     // ---- the wavefronts of the same rows meet: each brings its sums to the largest reference among them
-    l += __shfl_xor(l, 16, WAVE);
-    l += __shfl_xor(l, 32, WAVE);
+    l = of_quarters(l, sum_of());
     if (c == 0) {
         m_sh[wave][r] = m;
         l_sh[wave][r] = l;
@@ -478,7 +480,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
                 if (((any >> (16 * k)) & 0xffffu) == 0) continue;
                 const int bi = b * 16 + wave * 4 + k, tok = rows.token(bi), head = rows.head(bi);
                 float em, el, eo[D / 64];
-                exact_row<D, FP8>(a.q + (size_t)(rq.row0 + tok) * a.ld_q + head * D, sc, rq.P + tok, kb0, kb1, tile_at, em, el, eo);
+                exact_row<D, FP8>(a.q + (size_t)(rq.row0 + tok) * a.ld_q + head * D, sc, rq.P + tok, kb0, kb0 + held, tile_at, em, el, eo);
                 bf16* const bp = a.out + (size_t)(rq.row0 + tok) * a.ld_out + head * D;
 #pragma unroll
                 for (int j = 0; j < D / 64; ++j) {

@@ -2,6 +2,7 @@
 #pragma once
 #include "attend_few.h"
 #include "common.h"
+#include "lanes.h"
 
 typedef __attribute__((ext_vector_type(4))) int i32x4;
 
@@ -68,17 +69,13 @@ __global__ __launch_bounds__(256) void key_bounds_kernel(int n_req, int hkv, int
             hi[e] = fmaxf(hi[e], x);
             lo[e] = fminf(lo[e], x);
         }
-#pragma unroll
-        for (int off = CH; off < 64; off <<= 1) {
-            hi[e] = fmaxf(hi[e], __shfl_xor(hi[e], off, WAVE));
-            lo[e] = fminf(lo[e], __shfl_xor(lo[e], off, WAVE));
-        }
+        hi[e] = of_quarters(of_row<CH>(hi[e], larger_of()), larger_of());
+        lo[e] = of_quarters(of_row<CH>(lo[e], smaller_of()), smaller_of());
     }
     float top = 0.0f;
 #pragma unroll
     for (int e = 0; e < F; ++e) top = fmaxf(top, fmaxf(hi[e], -lo[e]));
-#pragma unroll
-    for (int off = 1; off < CH; off <<= 1) top = fmaxf(top, __shfl_xor(top, off, WAVE));
+    top = of_row<1>(top, larger_of());
     const int ex = code_exponent(top);
     int8_t* const codes = reinterpret_cast<int8_t*>(rq.codes) + ((size_t)h * rq.room + block) * 2 * D;
     if (lane < CH) {
@@ -100,7 +97,7 @@ __global__ __launch_bounds__(256) void key_bounds_kernel(int n_req, int hkv, int
 // ---------------------------------------------------------------- selection
 // One workgroup per (KV head, a few consecutive tokens of a request).
 //  1. every token's p and n (see the score in the header), int8, into LDS;
-//  2. scores of 16 blocks x 16 tokens per v_mfma_i32_16x16x64_i8 chain (the contraction runs over high and low codes), as keys
+//  2. scores of 16 blocks x 4 tokens (of 16 it has room for) per v_mfma_i32_16x16x64_i8 chain (the contraction runs over high and low codes), as keys
 //     that order like the scores, into LDS;
 //  3. a team per token finds the score that the last selected block has, digit by digit of the keys' range (a histogram in LDS per
 //     digit: integers, in any order the same), and writes the blocks down in ascending order.
@@ -139,13 +136,13 @@ RS_DEVICE uint32_t key_of_score(float s) {
 
 // What a team shares in LDS.
 template <int TEAM>
-struct SelectTeam {
-    uint32_t hist[256];
-    uint32_t digit, left, done;      // of a digit's search
+struct alignas(16) SelectTeam {
+    uint32_t hist[4 * 256];          // of each digit's search
     uint32_t low[TEAM], high[TEAM];
 };
 
-// A key that exactly `take` of key[lo .. hi) are above, 0 < take < hi - lo, but for *equals of those equal to it.  TEAM wavefronts.
+// A key that exactly `take` of key[lo .. hi) are above, 0 < take < hi - lo, but for *equals of those equal to it.  TEAM wavefronts, which
+// count together and then all find the digit from the counts.
 template <int TEAM>
 RS_DEVICE uint32_t cut_of_keys(const uint32_t* key, int lo, int hi, int take, SelectTeam<TEAM>& sh, int* equals) {
     const int lane = threadIdx.x & 63, member = TEAM == 1 ? lane : (int)threadIdx.x, wave = TEAM == 1 ? 0 : (int)threadIdx.x >> 6;
@@ -153,74 +150,56 @@ RS_DEVICE uint32_t cut_of_keys(const uint32_t* key, int lo, int hi, int take, Se
         if constexpr (TEAM > 1) __syncthreads();
         else __builtin_amdgcn_wave_barrier();   // (one wavefront's LDS accesses are in order)
     };
+    for (int i = member; i < 256; i += 64 * TEAM) *reinterpret_cast<uint4*>(&sh.hist[i * 4]) = make_uint4(0u, 0u, 0u, 0u);
     uint32_t low = 0xffffffffu, high = 0u;
     for (int b = lo + member; b < hi; b += 64 * TEAM) {
         low = min(low, key[b]);
         high = max(high, key[b]);
     }
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) {
-        low = min(low, (uint32_t)__shfl_xor((int)low, off, WAVE));
-        high = max(high, (uint32_t)__shfl_xor((int)high, off, WAVE));
-    }
+    low = of_wave(low, smaller_of());
+    high = of_wave(high, larger_of());
     if constexpr (TEAM > 1) {
         if (lane == 0) {
             sh.low[wave] = low;
             sh.high[wave] = high;
         }
         __syncthreads();
-#pragma unroll
-        for (int w = 0; w < TEAM; ++w) {
-            low = min(low, sh.low[w]);
-            high = max(high, sh.high[w]);
-        }
+        low = of_row<1>(sh.low[lane % TEAM], smaller_of());   // (a row of lanes has them all)
+        high = of_row<1>(sh.high[lane % TEAM], larger_of());
+        static_assert(TEAM <= 16, "a row of lanes");
     }
+    low = __builtin_amdgcn_readfirstlane(low);
+    high = __builtin_amdgcn_readfirstlane(high);
     uint32_t prefix = 0, left = (uint32_t)take;
     int top = high == low ? 0 : 32 - __builtin_clz(high - low);   // bits of key - low that are not known yet
-    bool first = true;
-    while (top > 0) {
+    for (int digit = 0; top > 0; ++digit) {
         const int shift = max(top - 8, 0);
         const uint32_t mask = (1u << (top - shift)) - 1u;
-        if (member < 64) *reinterpret_cast<uint4*>(&sh.hist[member * 4]) = make_uint4(0u, 0u, 0u, 0u);
+        uint32_t* const hist = sh.hist + digit * 256;
         meet();
         for (int b = lo + member; b < hi; b += 64 * TEAM) {
             const uint32_t x = key[b] - low;
-            if (first || (x >> top) == prefix) atomicAdd(&sh.hist[(x >> shift) & mask], 1u);
+            if (digit == 0 || (x >> top) == prefix) atomicAdd(&hist[(x >> shift) & mask], 1u);
         }
         meet();
-        if (wave == 0) {   // lane: digits 4 lane .. 4 lane + 3, counted from the largest
-            const uint4 h = *reinterpret_cast<const uint4*>(&sh.hist[lane * 4]);
-            const uint32_t mine = h.x + h.y + h.z + h.w;
-            uint32_t sum = mine;   // of this lane's digits and all larger ones
+        // lane: digits 4 lane .. 4 lane + 3, counted from the largest
+        const uint4 h = *reinterpret_cast<const uint4*>(&hist[lane * 4]);
+        const uint32_t mine = h.x + h.y + h.z + h.w, sum = sum_from_lane(mine), above = sum - mine;
+        uint32_t rest = left - above, d = 3;   // (of the one lane that has the digit)
+        const uint32_t count[4] = {h.x, h.y, h.z, h.w};
 #pragma unroll
-            for (int off = 1; off < 64; off <<= 1) {
-                const uint32_t up = (uint32_t)__shfl_down((int)sum, off, WAVE);
-                if (lane + off < 64) sum += up;
+        for (int i = 3; i > 0; --i)
+            if (d == (uint32_t)i && rest > count[i]) {
+                rest -= count[i];
+                d = i - 1;
             }
-            const uint32_t above = sum - mine;
-            if (above < left && left <= sum) {   // (one lane)
-                uint32_t rest = left - above, d = 3;
-                const uint32_t count[4] = {h.x, h.y, h.z, h.w};
-#pragma unroll
-                for (int i = 3; i > 0; --i)
-                    if (d == (uint32_t)i && rest > count[i]) {
-                        rest -= count[i];
-                        d = i - 1;
-                    }
-                const uint32_t in_digit = d == 3 ? h.w : d == 2 ? h.z : d == 1 ? h.y : h.x;
-                sh.digit = (uint32_t)lane * 4 + d;
-                sh.left = rest;
-                sh.done = rest == in_digit;   // (all of that digit belong: nothing below it matters)
-            }
-        }
-        meet();
-        prefix = (prefix << (top - shift)) | sh.digit;
-        left = sh.left;
+        const uint32_t in_digit = d == 3 ? h.w : d == 2 ? h.z : d == 1 ? h.y : h.x;
+        const int who = (int)__builtin_ctzll(__builtin_amdgcn_ballot_w64(above < left && left <= sum));
+        left = __builtin_amdgcn_readlane(rest, who);
+        prefix = (prefix << (top - shift)) | ((uint32_t)who * 4 + __builtin_amdgcn_readlane(d, who));
         top = shift;
-        first = false;
-        const bool done = sh.done != 0;
-        meet();
-        if (done && top > 0) {   // all from the digit's smallest key on; (prefix << top is not 0: some keys are left out)
+        if (top > 0 && left == (uint32_t)__builtin_amdgcn_readlane(in_digit, who)) {
+            // all of that digit belong: all from its smallest key on; (prefix << top is not 0: some keys are left out)
             *equals = 0;
             return low + (prefix << top) - 1u;
         }
@@ -237,7 +216,7 @@ __global__ __launch_bounds__(STEPS == SELECT_FROM_SCORES ? 1024 : 256) void bloc
     static_assert(WIDE || STEPS == SELECT_ALL, "only few tokens take two launches");
     constexpr int WAVES = STEPS == SELECT_FROM_SCORES ? 16 : 4, TEAM = WIDE ? WAVES : 1, TEAMS = WAVES / TEAM, KK = 2 * D / 64, U = SELECT_U;
     extern __shared__ __attribute__((aligned(16))) uint32_t keys[];   // [tokens][blocks]
-    __shared__ __attribute__((aligned(16))) int8_t u[16][2 * D];
+    __shared__ __attribute__((aligned(16))) int8_t u[4][2 * D];
     __shared__ __attribute__((aligned(16))) SelectTeam<TEAM> team_sh[TEAMS];
     __shared__ uint32_t chunk_more[TEAM == 1 ? 1 : SELECT_MAX_BLOCKS / 64], chunk_equal[TEAM == 1 ? 1 : SELECT_MAX_BLOCKS / 64];
     const uint32_t* const table = tab.w;
@@ -267,77 +246,74 @@ __global__ __launch_bounds__(STEPS == SELECT_FROM_SCORES ? 1024 : 256) void bloc
         const int8_t* const codes = reinterpret_cast<const int8_t*>(rq.codes) + (size_t)h * rq.room * 2 * D;
         const float* const units = reinterpret_cast<const float*>(rq.units) + (size_t)h * rq.room;
         i32x4 x[U][KK];
-        float unit[U][4];
+        float unit[U];
         const auto load = [&](int b) RS_INLINE {   // bounds of the wavefront's blocks b ..
 #pragma unroll
             for (int v = 0; v < U; ++v) {
-                const int8_t* const src = codes + (size_t)min(b + v * 16 + r, s1 - 1) * 2 * D + c * 16;
+                const int block = min(b + v * 16 + r, s1 - 1);
+                const int8_t* const src = codes + (size_t)block * 2 * D + c * 16;
 #pragma unroll
                 for (int k = 0; k < KK; ++k) x[v][k] = *reinterpret_cast<const i32x4*>(src + k * 64);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) unit[v][e] = units[min(b + v * 16 + c * 4 + e, s1 - 1)];
+                unit[v] = units[block];
             }
         };
+        // a wavefront's token, eight heads at a time, their loads in flight together and before the bounds'
+        const bf16* const query = a.q + (size_t)(rq.row0 + t0 + min(wave, nt - 1)) * a.ld_q + (size_t)h * a.g * D + lane * W;
+        typedef __attribute__((ext_vector_type(W))) __bf16 heads_t;
+        heads_t qh[8];
+        const auto load_heads = [&](int i0) RS_INLINE {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) qh[i] = *reinterpret_cast<const heads_t*>(query + (size_t)min(i0 + i, a.g - 1) * D);
+        };
+        load_heads(0);
         int b = s0 + share * SELECT_ROUND + wave * 16 * U;
         load(b);   // (under way while the queries become codes)
-        for (int t = wave; t < 16; t += WAVES) {
+        if (wave < nt) {
             int p[W] = {}, n[W] = {};
-            if (t < nt) {
-                const bf16* const src = a.q + (size_t)(rq.row0 + t0 + t) * a.ld_q + (size_t)h * a.g * D + lane * W;
-                // eight heads at a time, their loads in flight together
-                float top = 0.0f;
-                for (int i0 = 0; i0 < a.g; i0 += 8) {
-                    float x[8][W];
+            float top = 0.0f;
+            for (int i0 = 0;;) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
+                for (int i = 0; i < 8; ++i)
 #pragma unroll
-                        for (int j = 0; j < W; ++j) x[i][j] = bf16_to_f32(src[min(i0 + i, a.g - 1) * D + j]);
+                    for (int j = 0; j < W; ++j) top = fmaxf(top, fabsf(limited((float)qh[i][j])));
+                i0 += 8;
+                if (i0 >= a.g) break;
+                load_heads(i0);
+            }
+            const int ex = code_exponent(of_wave(top, larger_of()));
+            for (int i0 = 0; i0 < a.g; i0 += 8) {
+                if (a.g > 8) load_heads(i0);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
+                for (int i = 0; i < 8; ++i)
 #pragma unroll
-                        for (int j = 0; j < W; ++j) top = fmaxf(top, fabsf(limited(x[i][j])));
-                }
-#pragma unroll
-                for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, WAVE));
-                const int ex = code_exponent(top);
-                for (int i0 = 0; i0 < a.g; i0 += 8) {
-                    float x[8][W];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-#pragma unroll
-                        for (int j = 0; j < W; ++j) x[i][j] = bf16_to_f32(src[min(i0 + i, a.g - 1) * D + j]);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-#pragma unroll
-                        for (int j = 0; j < W; ++j) {
-                            const int code = i0 + i < a.g ? (int)rintf(__builtin_ldexpf(limited(x[i][j]), -ex)) : 0;
-                            p[j] += max(code, 0);
-                            n[j] += max(-code, 0);
-                        }
-                }
+                    for (int j = 0; j < W; ++j) {
+                        const int code = i0 + i < a.g ? (int)rintf(__builtin_ldexpf(limited((float)qh[i][j]), -ex)) : 0;
+                        p[j] += max(code, 0);
+                        n[j] += max(-code, 0);
+                    }
             }
             const int half = (1 << a.halvings) >> 1;
 #pragma unroll
             for (int j = 0; j < W; ++j) {
-                u[t][lane * W + j] = (int8_t)((p[j] + half) >> a.halvings);
-                u[t][D + lane * W + j] = (int8_t)(-((n[j] + half) >> a.halvings));
+                u[wave][lane * W + j] = (int8_t)((p[j] + half) >> a.halvings);
+                u[wave][D + lane * W + j] = (int8_t)(-((n[j] + half) >> a.halvings));
             }
         }
         __syncthreads();
-        i32x4 uf[KK];
+        i32x4 uf[KK];   // (rows past the tokens' are not used)
 #pragma unroll
-        for (int k = 0; k < KK; ++k) uf[k] = *reinterpret_cast<const i32x4*>(&u[r][k * 64 + c * 16]);
+        for (int k = 0; k < KK; ++k) uf[k] = *reinterpret_cast<const i32x4*>(&u[WIDE ? 0 : r & 3][k * 64 + c * 16]);
         while (b < s1) {
 #pragma unroll
             for (int v = 0; v < U; ++v) {
                 i32x4 dot = {0, 0, 0, 0};
 #pragma unroll
-                for (int k = 0; k < KK; ++k) dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[v][k], uf[k], dot, 0, 0, 0);
+                for (int k = 0; k < KK; ++k) dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(uf[k], x[v][k], dot, 0, 0, 0);
+                const int block = b + v * 16 + r;   // token 4 c + e
+                if (c == 0 && block < s1)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {   // block b + 16 v + 4 c + e, token r
-                    const int block = b + v * 16 + c * 4 + e;
-                    if (r < nt && block < s1) to[r * a.blocks + block - s0] = key_of_score((float)dot[e] * unit[v][e]);
-                }
+                    for (int e = 0; e < (WIDE ? 1 : 4); ++e)
+                        if (e < nt) to[e * a.blocks + block - s0] = key_of_score((float)dot[e] * unit[v]);
             }
             b += split * SELECT_ROUND;
             if (b < s1) load(b);
@@ -395,11 +371,8 @@ __global__ __launch_bounds__(STEPS == SELECT_FROM_SCORES ? 1024 : 256) void bloc
                     more += (int)chunk_more[i];
                     equal += (int)chunk_equal[i];
                 }
-#pragma unroll
-                for (int off = 32; off > 0; off >>= 1) {
-                    more += __shfl_xor(more, off, WAVE);
-                    equal += __shfl_xor(equal, off, WAVE);
-                }
+                more = of_wave(more, sum_of());
+                equal = of_wave(equal, sum_of());
                 bool eq;
                 bool sel = taken(ch * 64 + lane, eq);
                 if (eq) sel = equal + (int)__popcll(__builtin_amdgcn_ballot_w64(eq) & below) < equals;

@@ -31,10 +31,11 @@ namespace {
 // KV heads times tiles, all together, up to these.  The chunk kernel needs its descriptors in the workspace first (a launch), a merge more often,
 // and 8-bit caches expanded.  us a pass, chunk kernel / attend_few_kernel, 28 query heads, 4 KV heads: 64 tokens on 2000 (896 of them)
 // 20.4 / 17.5, 96 on 2000 (1408) 22.5 / 23.5, 32 on 8000 (2000) 23.1 / 26.3, 12 on 30000 (3752) 37.9 / 43.4; 64 heads, 8 KV heads: 32 on 2000
-// (1024) 20.2 / 19.8, 48 (1536) 22.3 / 24.1; 8 bits: 128 on 2000 (1792) 31.3 / 22.8, 128 on 8000 (7000) 39.0 / 38.8, 48 on 30000 (11256)
-// 58.3 / 58.8.
+// (1024) 20.2 / 19.8, 48 (1536) 22.3 / 24.1; beside 23 single tokens on 3000, where its launches come on top: 28 and 4 heads, 12 on 5000 (632)
+// 51.2 / 44.7, 48 on 4000 (1512) 54.8 / 42.8; 64 and 8, 12 on 5000 (1264) 75.6 / 74.7, 24 on 4000 (1512) 76.3 / 82.2; 8 bits: 128 on 2000
+// (1792) 31.3 / 22.8, 128 on 8000 (7000) 39.0 / 38.8, 48 on 30000 (11256) 58.3 / 58.8.
 constexpr int FEW_ROWS = FEW_GROUP;
-constexpr long FEW_TILES = 1100, FEW_TILES_FP8 = 8000;
+constexpr long FEW_TILES = 1400, FEW_TILES_FP8 = 8000;
 // Caches that one call reads once are loaded with the streaming hint, unless they are so small that the L2s may still have them from a call
 // before.  us with / without it, behind a fill of 1 GB: 8 MB 14.6 / 15.6, 35 MB 19.6 / 26.6, 141 MB 38.3 / 69.5; call after call on the
 // same caches: 4 MB 15.7 / 14.6, 8 MB 20.2 / 20.4, 141 MB 53.3 / 54.5.
