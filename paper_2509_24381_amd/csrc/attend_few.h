@@ -258,13 +258,15 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
     float m = -INFINITY, l = 0.0f;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) acc[dt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    // ---- this wavefront's share of the tiles; their places (page or block) in a register, a lane each, 64 at a time.  (Neighbours, so that page
-    // numbers read across the host link are few lines.)
-    const int first = kb0 + held / sharers * share + min(share, held % sharers), own = held / sharers + (share < held % sharers);
-    const int tiles = rb * 16 < rows.rows ? own : 0, last = max(first + own - 1, 0);
+    // ---- this wavefront's share of the tiles: neighbours, so that page numbers read across the host link are few lines; of a list every
+    // sharers-th, so that wavefronts all over the chip pass the same blocks at about the same time and find them in the L2s.  Their places
+    // (page or block) are in a register, a lane each, 64 at a time.
+    const int own = held / sharers + (share < held % sharers);
+    const int first = kb0 + (LIST ? share : held / sharers * share + min(share, held % sharers)), stride = LIST ? sharers : 1;
+    const int tiles = rb * 16 < rows.rows ? own : 0, last = first + max(own - 1, 0) * stride;
     int place = 0, number = 0;
     const auto look_up = [&](int j0) RS_INLINE {   // of tiles j0 .. j0 + 63
-        const int i = min(first + j0 + lane, last);
+        const int i = min(first + (j0 + lane) * stride, last);
         number = LIST ? list[i] : i;
         place = rq.pages == CONTIGUOUS ? number : (int)pages[rq.pages + number];
     };
