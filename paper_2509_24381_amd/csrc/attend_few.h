@@ -47,7 +47,7 @@ struct FewReq {
     int32_t parts;         // parts of the key range
     int32_t slot0;         // of its first part
     float k_scale, v_scale;
-    int32_t pad_;
+    int32_t once;          // nothing of it that is read is read again soon
 };
 constexpr int REQ_WORDS = 12;
 static_assert(sizeof(FewReq) == 4 * REQ_WORDS, "REQ_WORDS");
@@ -174,9 +174,8 @@ struct FewUnit {
     RS_UNIT static uint32_t v_source(int lane) { return v_place(lane / (V_ROW / 16), lane % (V_ROW / 16)); }
 };
 
-// ONCE: nothing that is read is read again soon.
 constexpr int FEW_ONCE = 2;   // cache policy (nt)
-template <int D, bool FP8, bool LIST, bool ONCE, bool INLINE>
+template <int D, bool FP8, bool LIST, bool INLINE>
 __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a, std::conditional_t<INLINE, InlineTable, NoTable> tab) {
     typedef FewUnit<D, FP8> U;
     constexpr int KS = D / 32, DT = D / 16, NT = U::SUBS, DTU = DT / U::PER;   // sub-tiles of a K unit, feature blocks of a V unit
@@ -284,12 +283,17 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
         const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
             (void*)((keys ? k_head : v_head) + (uint64_t)(uint32_t)__builtin_amdgcn_readlane(place, j & 63) * place_bytes), 0, U::TILE, 0x00020000);
         char* const to = mine + (h & 1) * U::BYTES;
+        const auto load = [&](auto policy) RS_INLINE {
 #pragma unroll
-        for (int i = 0; i < U::LOADS; ++i) {
-            const uint32_t from = keys ? k_src[i] : v_src;   // (named: template-dependent arguments of the builtin break the host-side stub)
-            const int further = keys ? U::k_start(h, i) : h % U::PER * U::BYTES + i * 1024;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)(uintptr_t)(uint32_t)(uintptr_t)(to + i * 1024), 16, from, further, 0, ONCE ? FEW_ONCE : 0);
-        }
+            for (int i = 0; i < U::LOADS; ++i) {
+                const uint32_t from = keys ? k_src[i] : v_src;   // (named: template-dependent arguments of the builtin break the host-side stub)
+                const int further = keys ? U::k_start(h, i) : h % U::PER * U::BYTES + i * 1024;
+                constexpr int aux = decltype(policy)::value;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)(uintptr_t)(uint32_t)(uintptr_t)(to + i * 1024), 16, from, further, 0, aux);
+            }
+        };
+        if (!LIST && rq.once) load(std::integral_constant<int, FEW_ONCE>{});
+        else load(std::integral_constant<int, 0>{});
     };
     // (the compiler does not see LDS written by DMA, nor may it move a refill above the reads of what it overwrites)
     const auto wait_loads = [&](bool others) RS_INLINE {   // others: U::LOADS younger ones may be in flight

@@ -215,22 +215,28 @@ size_t expansion_bytes(const rs_ctx* c, long tokens) { return (size_t)2 * align_
 // ---------------------------------------------------------------- few rows
 // Parts of the key ranges, of `len` tiles at most.  Estimated in tiles of a place (a workgroup's room on a compute unit) when all places stream:
 // an item costs 1.5 beside its tiles, joining 2.  With no more items than places the longest ends last, but the fewer are left the
-// faster they stream: a tile then takes 0.66 of one (more where several wavefronts need every tile: 16 rows each).  With more, the last
-// ones start late: a share of the longest comes on top.  us a pass, parts of 4 / 8 / 16 / 24 / 48 tiles: 64 requests on up to 8000 tokens
+// faster they stream: a tile then takes 0.66 of one.  With more, the last ones start late: a share of the longest comes on top.  Where two or
+// all four wavefronts need every tile (16 rows each) it takes 2 and 3 times as long, and parts are that much shorter (us a pass, all
+// alike -> so: 30 single tokens on up to 8000 beside 4 requests of 5 on 3000, 64 query heads, 8 KV heads, 142.7 -> 115.5, 8 bits
+// 91.3 -> 55.8; 24 requests of 3 on up to 6000 beside one of 12 on 5000 68.4 -> 53.4; one of 4 on 8000, alone, 15.8 -> 17.2).  us a pass, parts of 4 / 8 / 16 / 24 / 48 tiles: 64 requests on up to 8000 tokens
 // 100.5 / 93.8 / 88.7 / 92.2 / 90.1; 16 on up to 32000, 8 bits, 82.8 / 77.6 / 70.6 / 67.6 / 61.1; 24 of 3 tokens on up to 6000, 8 query
 // heads per KV head, 77.5 / 73.2 / 72.4 / 87.2 / 99.7.
 struct FewRequest {
     int kv, row0, T;       // index into kvs, first row, rows
     int units, tiles;      // items per part, tiles
-    int row_blocks;        // of 16 rows
+    int row_blocks;        // of 16 rows: 1, 2 or 4
     int parts;
+    bool once = false;     // its tiles are read once
+    int weight() const { return row_blocks == 1 ? 1 : row_blocks == 2 ? 2 : 3; }   // of a tile
+    long work() const { return (long)tiles * weight(); }
+    int parts_of(int len) const { return (int)std::min<long>((work() + len - 1) / len, FEW_MAX_PARTS); }
 };
 void plan_few(std::vector<FewRequest>& reqs, int places, size_t slots) {
     long total = 0;
     int longest = 1;
     for (const FewRequest& r : reqs) {
-        total += (long)r.units * r.tiles;
-        longest = std::max(longest, r.tiles);
+        total += r.units * r.work();
+        longest = std::max(longest, (int)r.work());
     }
     double best = 1e30;
     int best_len = longest;
@@ -238,10 +244,10 @@ void plan_few(std::vector<FewRequest>& reqs, int places, size_t slots) {
         long items = 0, split = 0;
         double most = 0.0;
         for (const FewRequest& r : reqs) {
-            const int p = std::min((r.tiles + len - 1) / len, FEW_MAX_PARTS);
+            const int p = r.parts_of(len);
             items += (long)r.units * p;
             if (p > 1) split += (long)r.units * p * r.row_blocks;
-            most = std::max(most, ((r.tiles + p - 1) / p) * (r.row_blocks == 1 ? 0.66 : r.row_blocks == 2 ? 0.85 : 1.1));
+            most = std::max(most, (r.tiles + p - 1) / p * r.weight() * 0.66);
         }
         const double share = (double)total / places;
         const double cost = (items <= places ? std::max(share, most) + 1.5 : share + 1.5 * items / places + 0.5 * most) + (split ? 2.0 : 0.0);
@@ -251,7 +257,7 @@ void plan_few(std::vector<FewRequest>& reqs, int places, size_t slots) {
         }
         if (len >= longest) break;
     }
-    for (FewRequest& r : reqs) r.parts = std::min((r.tiles + best_len - 1) / best_len, FEW_MAX_PARTS);
+    for (FewRequest& r : reqs) r.parts = r.parts_of(best_len);
 }
 
 // The table of `reqs` at `w` (`words` of room, checked by the caller), their page numbers at `pages`.  LIST: items are rows.
@@ -276,6 +282,7 @@ FewTable write_few_table(const rs_ctx* ctx, int layer, rs_kv* const* kvs, const 
         }
         q.row0 = r.row0; q.T = r.T; q.P = kv->len[layer] - r.T;
         q.parts = r.parts;
+        q.once = r.once;
         q.slot0 = list ? 0 : slot;
         q.k_scale = kv->k_scale; q.v_scale = kv->v_scale;
         memcpy(&w[table_reqs_at(n) + REQ_WORDS * j], &q, sizeof(q));
@@ -298,20 +305,18 @@ size_t few_table_pages(rs_kv* const* kvs, const std::vector<FewRequest>& reqs) {
 }
 
 template <bool LIST>
-rs_status launch_few(const rs_ctx* ctx, bool fp8, bool once, const FewArgs& a, uint32_t items, uint32_t units, bool split, const InlineTable* tab, hipStream_t st) {
+rs_status launch_few(const rs_ctx* ctx, bool fp8, const FewArgs& a, uint32_t items, uint32_t units, bool split, const InlineTable* tab, hipStream_t st) {
     for_kind(ctx, fp8, [&](auto d, auto f8) {
         constexpr int D = decltype(d)::value;
         constexpr bool FP8 = decltype(f8)::value;
         if constexpr (LIST) {
-            hipLaunchKernelGGL((attend_few_kernel<D, FP8, true, false, false>), dim3(items), dim3(64 * FEW_WAVES), 0, st, a, NoTable{});
+            hipLaunchKernelGGL((attend_few_kernel<D, FP8, true, false>), dim3(items), dim3(64 * FEW_WAVES), 0, st, a, NoTable{});
             if (split) hipLaunchKernelGGL((few_merge_kernel<D, true, false>), dim3(units, D / 32), dim3(256), 0, st, a, NoTable{});
         } else if (tab) {
-            if (once) hipLaunchKernelGGL((attend_few_kernel<D, FP8, false, true, true>), dim3(items), dim3(64 * FEW_WAVES), 0, st, a, *tab);
-            else hipLaunchKernelGGL((attend_few_kernel<D, FP8, false, false, true>), dim3(items), dim3(64 * FEW_WAVES), 0, st, a, *tab);
+            hipLaunchKernelGGL((attend_few_kernel<D, FP8, false, true>), dim3(items), dim3(64 * FEW_WAVES), 0, st, a, *tab);
             if (split) hipLaunchKernelGGL((few_merge_kernel<D, false, true>), dim3(units, D / 32), dim3(256), 0, st, a, *tab);
         } else {
-            if (once) hipLaunchKernelGGL((attend_few_kernel<D, FP8, false, true, false>), dim3(items), dim3(64 * FEW_WAVES), 0, st, a, NoTable{});
-            else hipLaunchKernelGGL((attend_few_kernel<D, FP8, false, false, false>), dim3(items), dim3(64 * FEW_WAVES), 0, st, a, NoTable{});
+            hipLaunchKernelGGL((attend_few_kernel<D, FP8, false, false>), dim3(items), dim3(64 * FEW_WAVES), 0, st, a, NoTable{});
             if (split) hipLaunchKernelGGL((few_merge_kernel<D, false, false>), dim3(units, D / 32), dim3(256), 0, st, a, NoTable{});
         }
     });
@@ -631,12 +636,9 @@ rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, 
     InlineTable tab;
     enum { NOTHING, PAGES, ALL } few_staged = NOTHING;   // of the table (see TABLE_WORDS)
     size_t few_words = 0, few_bytes = 0;   // few_bytes: of the keys and values they read
-    bool once = true;                      // nobody reads them twice
     if (!few.empty()) {
-        for (const FewRequest& r : few) {
-            few_bytes += (size_t)r.tiles * 128 * ctx->kv_dim * (fp8 ? 1 : 2);
-            once &= r.units == f.n_kv_heads;
-        }
+        for (const FewRequest& r : few) few_bytes += (size_t)r.tiles * 128 * ctx->kv_dim * (fp8 ? 1 : 2);
+        for (FewRequest& r : few) r.once = few_bytes >= FEW_ONCE_BYTES && r.row_blocks == 1;
         plan_few(few, FEW_PLACES * ctx->n_cu, SLOT_ROWS / 16);
         a.n_req = (int)few.size();
         a.hkv = f.n_kv_heads; a.g = ctx->group;
@@ -725,7 +727,7 @@ rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, 
         if (a.pages) a.pages = reinterpret_cast<const uint32_t*>(ws);   // (copied too)
     }
     if (!few.empty() &&
-        (s = launch_few<false>(ctx, fp8, once && few_bytes >= FEW_ONCE_BYTES, a, ft.items, ft.units, ft.any_split, few_staged == ALL ? nullptr : &tab, st)) != RS_OK)
+        (s = launch_few<false>(ctx, fp8, a, ft.items, ft.units, ft.any_split, few_staged == ALL ? nullptr : &tab, st)) != RS_OK)
         return s;
     if (staged && (s = ring_commit(ctx, st)) != RS_OK) return s;
     if (!chunks) return RS_OK;
@@ -910,7 +912,7 @@ rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int*
     a.chosen = list;
     a.n_blocks = n_blocks;
     a.list_parts = parts;
-    return launch_few<true>(ctx, fp8, false, a, (uint32_t)(units * parts), (uint32_t)(units * rbn), parts > 1, nullptr, st);
+    return launch_few<true>(ctx, fp8, a, (uint32_t)(units * parts), (uint32_t)(units * rbn), parts > 1, nullptr, st);
 }
 
 }  // extern "C"
