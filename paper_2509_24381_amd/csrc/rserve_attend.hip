@@ -28,14 +28,16 @@ struct rs_rotary {
 namespace {
 
 // Requests of up to 64 stacked rows go to attend_few_kernel, and so do the others of a call if they have little to read: their row groups times
-// KV heads times tiles, all together, up to these.  The chunk kernel needs its descriptors in the workspace first (a launch), a merge more often,
-// and 8-bit caches expanded.  us a pass, chunk kernel / attend_few_kernel, 28 query heads, 4 KV heads: 64 tokens on 2000 (896 of them)
-// 20.4 / 17.5, 96 on 2000 (1408) 22.5 / 23.5, 32 on 8000 (2000) 23.1 / 26.3, 12 on 30000 (3752) 37.9 / 43.4; 64 heads, 8 KV heads: 32 on 2000
-// (1024) 20.2 / 19.8, 48 (1536) 22.3 / 24.1; beside 23 single tokens on 3000, where its launches come on top: 28 and 4 heads, 12 on 5000 (632)
-// 51.2 / 44.7, 48 on 4000 (1512) 54.8 / 42.8; 64 and 8, 12 on 5000 (1264) 75.6 / 74.7, 24 on 4000 (1512) 76.3 / 82.2; 8 bits: 128 on 2000
-// (1792) 31.3 / 22.8, 128 on 8000 (7000) 39.0 / 38.8, 48 on 30000 (11256) 58.3 / 58.8.
+// KV heads times tiles, all together, up to FEW_TILES; beside requests of few rows, where the chunk kernel's launches come on top of those, up
+// to FEW_TILES_BESIDE; with 8-bit caches, which the chunk kernel needs expanded, up to FEW_TILES_FP8.  us a pass, chunk kernel /
+// attend_few_kernel, (g) 28 query and 4 KV heads, (h) 64 and 8.  One request: (g) 64 tokens on 2000 (896 row groups x heads x tiles)
+// 20.8 / 19.4, 96 on 2000 (1408) 23.0 / 22.0, 96 on 4000 (2772) 26.7 / 28.2, 12 on 20000 (2504) 31.6 / 25.2; (h) 12 on 8000 (2000) 22.9 / 22.2,
+// 32 on 6000 (3008) 26.1 / 28.7, 100 on 2000 (3328) 26.1 / 31.2.  Beside 23 single tokens on 3000: (g) 12 on 5000 (632) 51.4 / 36.9, 24 on 20000
+// (3756) 65.1 / 52.3; (h) 48 on 4000 (3024) 79.1 / 73.4, 24 on 20000 (7512) 93.0 / 94.6; beside 30 on 300: (g) 96 on 4000 (2772) 37.1 / 31.5, (h) 64
+// on 2000 (2048) 37.3 / 30.5, 96 on 4000 (6048) 45.1 / 57.5.  8 bits: (h) 12 on 16000 (4000) 46.5 / 26.8, 100 on 4000 (6552) 40.8 / 43.0; beside
+// 30 on 300, 96 on 4000 (6048) 48.4 / 46.2; beside 60 on 4000, 128 on 4000 (8064) 121.7 / 130.3.
 constexpr int FEW_ROWS = FEW_GROUP;
-constexpr long FEW_TILES = 1400, FEW_TILES_FP8 = 8000;
+constexpr long FEW_TILES = 2000, FEW_TILES_BESIDE = 4500, FEW_TILES_FP8 = 6000;
 // Caches that one call reads once are loaded with the streaming hint, unless they are so small that the L2s may still have them from a call
 // before.  us with / without it, behind a fill of 1 GB: 8 MB 14.6 / 15.6, 35 MB 19.6 / 26.6, 141 MB 38.3 / 69.5; call after call on the
 // same caches: 4 MB 15.7 / 14.6, 8 MB 20.2 / 20.4, 141 MB 53.3 / 54.5.
@@ -606,12 +608,15 @@ rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, 
     const auto row_groups = [&](int i) { return (stacked_rows(i) + FEW_GROUP - 1) / FEW_GROUP; };
     size_t expansion = 0;
     long tiles = 0;   // of the requests with more rows
-    for (int i = 0; i < R; ++i)
+    bool beside = false;
+    for (int i = 0; i < R; ++i) {
+        beside |= lens[i] > 0 && stacked_rows(i) <= FEW_ROWS;
         if (stacked_rows(i) > FEW_ROWS) {
             tiles += row_groups(i) * f.n_kv_heads * ((kvs[i]->len[layer] + 63) / 64);
             if (fp8) expansion += expansion_bytes(ctx, kvs[i]->len[layer]);
         }
-    const bool chunks = tiles > (ctx->few_tiles >= 0 ? ctx->few_tiles : fp8 ? FEW_TILES_FP8 : FEW_TILES);
+    }
+    const bool chunks = tiles > (ctx->few_tiles >= 0 ? ctx->few_tiles : fp8 ? FEW_TILES_FP8 : beside ? FEW_TILES_BESIDE : FEW_TILES);
     const auto is_few = [&](int i) { return lens[i] > 0 && (!chunks || stacked_rows(i) <= FEW_ROWS); };
     if (!chunks) expansion = 0;
     if ((s = check_workspace(workspace, workspace_bytes, L.total + expansion)) != RS_OK) return s;
