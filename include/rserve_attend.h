@@ -15,7 +15,9 @@
  * caches, and follow that header's conventions: device memory belongs to the caller, work is enqueued on the caller's stream,
  * errors are decided on the host before anything is launched or changed, nothing allocates device memory (rs_rotary_create
  * excepted, and HIP's own bookkeeping), no call may be captured into a HIP graph (RS_ESTATE), results do not depend on
- * the order in which workgroups run, one thread at a time per rs_ctx.
+ * the order in which workgroups run, one thread at a time per rs_ctx.  Calls that share a cache or a workspace are ordered by their stream;
+ * a caller that changes the stream between them orders the two with an event.  A call that finds no host memory returns RS_EHIP and
+ * leaves the cached tokens as they are.
  *
  * Rows.  q, k, v, q_out and out hold one row per new token, the tokens of request 0 first: sum of lens rows.  A row of q, q_out and
  * out is [Hq][d], of k and v [Hkv][d], bfloat16, contiguous; ld_* is the distance between rows in elements, so that q, k

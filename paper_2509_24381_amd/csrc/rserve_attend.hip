@@ -6,6 +6,8 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <exception>
+#include <memory>
 #include <vector>
 
 #include "attend_few.h"
@@ -375,6 +377,9 @@ rs_status launch_chunks(const rs_ctx* c, const AttnPlan& plan, const ReqDesc* d_
     return RS_OK;
 }
 
+// No exception may pass a C entry: the entries that allocate host memory end in this.
+rs_status not_allocated(const std::exception& e) { return fail(RS_EHIP, "no host memory: %s", e.what()); }
+
 }  // namespace
 
 size_t attend_staging_bytes(const rs_layer_cfg& cfg) { return attend_layout(cfg, cfg.max_tokens_per_call, cfg.max_requests, 0).tables; }
@@ -382,7 +387,7 @@ size_t attend_staging_bytes(const rs_layer_cfg& cfg) { return attend_layout(cfg,
 extern "C" {
 
 // =============================================================================================== rotary positions
-rs_status rs_rotary_create(rs_ctx* ctx, const rs_rotary_cfg* cfg, rs_rotary** out) {
+rs_status rs_rotary_create(rs_ctx* ctx, const rs_rotary_cfg* cfg, rs_rotary** out) try {
     if (!ctx || !cfg || !out) return fail(RS_EINVAL, "ctx / cfg / out is null");
     *out = nullptr;
     rs_rotary_cfg c = *cfg;
@@ -422,7 +427,7 @@ rs_status rs_rotary_create(rs_ctx* ctx, const rs_rotary_cfg* cfg, rs_rotary** ou
             freq[j] = f / c.factor * (1.0 - keep) + f * keep;
         }
     }
-    rs_rotary* r = new rs_rotary();
+    std::unique_ptr<rs_rotary, void (*)(rs_rotary*)> r(new rs_rotary(), rs_rotary_destroy);
     r->ctx = ctx;
     r->cfg = c;
     r->table.resize((size_t)c.max_pos * half);
@@ -434,13 +439,12 @@ rs_status rs_rotary_create(rs_ctx* ctx, const rs_rotary_cfg* cfg, rs_rotary** ou
     if (ctx->has_device) {
         hipError_t e = hipMalloc((void**)&r->table_dev, r->table.size() * sizeof(float2));
         if (e == hipSuccess) e = hipMemcpy(r->table_dev, r->table.data(), r->table.size() * sizeof(float2), hipMemcpyHostToDevice);
-        if (e != hipSuccess) {
-            rs_rotary_destroy(r);
-            return fail(RS_EHIP, "rotary table: %s", hipGetErrorString(e));
-        }
+        if (e != hipSuccess) return fail(RS_EHIP, "rotary table: %s", hipGetErrorString(e));
     }
-    *out = r;
+    *out = r.release();
     return RS_OK;
+} catch (const std::exception& e) {
+    return not_allocated(e);
 }
 
 void rs_rotary_destroy(rs_rotary* r) {
@@ -461,7 +465,7 @@ rs_status rs_rotary_at(const rs_rotary* r, int pos, int pair, float* cos_out, fl
 // =============================================================================================== append
 rs_status rs_kv_append(rs_ctx* ctx, const rs_rotary* rotary, int layer, rs_kv* const* kvs, const int* starts, const int* lens, int R,
                        const int* positions, const void* q, long ld_q, const void* k, long ld_k, const void* v, long ld_v, void* q_out, long ld_q_out,
-                       void* stream) {
+                       void* stream) try {
     long rows = 0;
     rs_status s = check_call(ctx, layer, kvs, lens, true, R, &rows);
     if (s != RS_OK) return s;
@@ -479,6 +483,8 @@ rs_status rs_kv_append(rs_ctx* ctx, const rs_rotary* rotary, int layer, rs_kv* c
             return fail(RS_ECAPACITY, "request %d: positions up to %ld exceed the rotary table's %d", i, after - 1, rotary->cfg.max_pos);
         if (kv->paged()) {
             const int missing = kv->pages_missing(layer, after);
+            std::vector<int>& held = kv->pages[layer];
+            if (held.capacity() < held.size() + missing) held.reserve(std::max(held.size() + missing, 2 * held.capacity()));
             auto it = std::find_if(need.begin(), need.end(), [&](const auto& e) { return e.first == kv->pool; });
             if (it == need.end()) need.emplace_back(kv->pool, missing);
             else it->second += missing;
@@ -502,8 +508,9 @@ rs_status rs_kv_append(rs_ctx* ctx, const rs_rotary* rotary, int layer, rs_kv* c
         if ((s = check_device(ctx)) != RS_OK) return s;
         if ((s = refuse_capture(st)) != RS_OK) return s;
     }
-    // from here on the call is made: tokens dropped, pages taken, launches
     std::vector<AppendItem> items;
+    items.reserve((size_t)rows / 64 + 2 * (size_t)R);
+    // from here on the call is made: tokens dropped, pages taken, launches
     int row = 0, longest = 0;
     const bool fp8 = R > 0 && kvs[0]->fp8;
     for (int i = 0; i < R; ++i) {
@@ -586,6 +593,8 @@ rs_status rs_kv_append(rs_ctx* ctx, const rs_rotary* rotary, int layer, rs_kv* c
         i0 = i1;
     }
     return RS_OK;
+} catch (const std::exception& e) {
+    return not_allocated(e);
 }
 
 // =============================================================================================== attention
@@ -596,7 +605,7 @@ size_t rs_attend_workspace_bytes(const rs_ctx* c, int max_rows, int max_requests
 }
 
 rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, int R, const void* q, long ld_q, void* out, long ld_out, float scale,
-                    void* workspace, size_t workspace_bytes, void* stream) {
+                    void* workspace, size_t workspace_bytes, void* stream) try {
     long rows = 0;
     rs_status s = check_attend(ctx, layer, kvs, lens, R, q, ld_q, out, ld_out, &scale, &rows);
     if (s != RS_OK) return s;
@@ -749,6 +758,8 @@ rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, 
     const bool paged = !pagetab.empty() && !fp8;
     if (f.head_dim == 128) return launch_chunks<128>(ctx, plan, d_reqs, d_items, d_mitems, paged, (const bf16*)q, ld_q, (bf16*)out, ld_out, scale_log2e, split_buf, st);
     return launch_chunks<64>(ctx, plan, d_reqs, d_items, d_mitems, paged, (const bf16*)q, ld_q, (bf16*)out, ld_out, scale_log2e, split_buf, st);
+} catch (const std::exception& e) {
+    return not_allocated(e);
 }
 
 // =============================================================================================== bounds
@@ -769,7 +780,7 @@ int rs_kv_bounded(const rs_kv* kv, int layer) {
     return kv->bounded[layer];
 }
 
-rs_status rs_kv_bounds_update(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* firsts, int R, void* stream) {
+rs_status rs_kv_bounds_update(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* firsts, int R, void* stream) try {
     rs_status s = check_call(ctx, layer, kvs, nullptr, false, R, nullptr);
     if (s != RS_OK) return s;
     std::vector<int> first(R);
@@ -788,11 +799,13 @@ rs_status rs_kv_bounds_update(rs_ctx* ctx, int layer, rs_kv* const* kvs, const i
     for (int i = 0; i < R; ++i)   // (with a gap before the first block the blocks after it do not count)
         if (first[i] <= kvs[i]->bounded[layer]) kvs[i]->bounded[layer] = kvs[i]->len[layer] / 64;
     return RS_OK;
+} catch (const std::exception& e) {
+    return not_allocated(e);
 }
 
 // =============================================================================================== attention over selected blocks
 rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, int R, const void* q, long ld_q, void* out, long ld_out,
-                           int n_blocks, int n_first, int n_last, float scale, int* chosen, void* workspace, size_t workspace_bytes, void* stream) {
+                           int n_blocks, int n_first, int n_last, float scale, int* chosen, void* workspace, size_t workspace_bytes, void* stream) try {
     long rows = 0;
     rs_status s = check_attend(ctx, layer, kvs, lens, R, q, ld_q, out, ld_out, &scale, &rows);
     if (s != RS_OK) return s;
@@ -918,6 +931,8 @@ rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int*
     a.n_blocks = n_blocks;
     a.list_parts = parts;
     return launch_few<true>(ctx, fp8, a, (uint32_t)(units * parts), (uint32_t)(units * rbn), parts > 1, nullptr, st);
+} catch (const std::exception& e) {
+    return not_allocated(e);
 }
 
 }  // extern "C"

@@ -5,6 +5,8 @@ Calls that pass all checks end in RS_EHIP here, before anything is launched or c
 import ctypes as C
 import os
 import re
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -225,3 +227,22 @@ def test_prepared_arguments_are_taken_as_they_are(ctx):
     cs, n = CacheSet([kv]), binding.int_array([3])
     refused("RS_EHIP", lambda: append(ctx, cs, n, n=3))
     assert binding.int_array(n) is n and len(cs) == 1
+
+
+def test_a_call_without_host_memory_is_refused():
+    """Address space is limited, in a process of its own: the table does not fit, and the call says so instead of ending the process."""
+    code = """
+import resource
+from paper_2509_24381_amd.binding import Context, LayerConfig, RotaryConfig, RsError
+ctx = Context(LayerConfig(hidden=256, n_q_heads=4, n_kv_heads=2, head_dim=64, mlp_inter=64, max_tokens_per_call=128, max_requests=4, max_pos=512))
+held = int(open('/proc/self/statm').read().split()[0]) * resource.getpagesize()
+resource.setrlimit(resource.RLIMIT_AS, (held + (2 << 30),) * 2)
+try:
+    ctx.rotary(RotaryConfig(rotary_dim=64, max_pos=1 << 28, theta=1e4))
+except RsError as e:
+    print(e.status_name, 'memory' in str(e))
+print(ctx.rotary(RotaryConfig(rotary_dim=64, max_pos=512, theta=1e4)).at(0, 0))
+"""
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0, r.stderr[-2000:]
+    assert r.stdout.splitlines() == ["RS_EHIP True", "(1.0, 0.0)"], r.stdout
