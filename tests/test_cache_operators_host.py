@@ -246,3 +246,9 @@ print(ctx.rotary(RotaryConfig(rotary_dim=64, max_pos=512, theta=1e4)).at(0, 0))
     r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=120)
     assert r.returncode == 0, r.stderr[-2000:]
     assert r.stdout.splitlines() == ["RS_EHIP True", "(1.0, 0.0)"], r.stdout
+
+
+def test_the_decode_command_needs_a_gpu():
+    from paper_2509_24381_amd import decode
+    with pytest.raises(SystemExit, match="GPU"):
+        decode.main([])
