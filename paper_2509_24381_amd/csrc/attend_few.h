@@ -72,9 +72,6 @@ RS_DEVICE int request_of(const uint32_t* table, int n_req, uint32_t id) {
     return __builtin_amdgcn_readfirstlane(at);
 }
 
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
-RS_DEVICE uint4 ld_tile_16(global_bytes p) { return __builtin_bit_cast(uint4, *reinterpret_cast<const __attribute__((address_space(1))) u32x4*>(p)); }
-
 // Eight E4M3 codes to bfloat16, exactly.
 RS_DEVICE bf16x8 bf16x8_of_codes(uint32_t lo, uint32_t hi) {
     bf16x8 o;

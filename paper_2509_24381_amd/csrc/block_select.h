@@ -5,6 +5,10 @@
 #include "lanes.h"
 
 typedef __attribute__((ext_vector_type(4))) int i32x4;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+RS_DEVICE uint4 ld_once_16(global_bytes p) {   // with the streaming hint
+    return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const __attribute__((address_space(1))) u32x4*>(p)));
+}
 
 constexpr float BOUND_LIMIT = 1.2676506002282294e30f;   // 2^100
 constexpr int BOUND_LEAST = -100;
@@ -48,7 +52,7 @@ __global__ __launch_bounds__(256) void key_bounds_kernel(int n_req, int hkv, int
     global_bytes kt = (global_bytes)(rq.k + (uint64_t)h * rq.head_bytes + index * rq.block_bytes);
     uint4 v[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = ld_tile_16(kt + (size_t)i * 1024 + lane * 16);
+    for (int i = 0; i < N; ++i) v[i] = ld_once_16(kt + (size_t)i * 1024 + lane * 16);   // (32768 tokens: 10.2 -> 9.8 us with the hint)
     const auto value = [&](const uint4& w, int e) RS_INLINE {
         const uint32_t x = e * (FP8 ? 1 : 2) / 4 == 0 ? w.x : e * (FP8 ? 1 : 2) / 4 == 1 ? w.y : e * (FP8 ? 1 : 2) / 4 == 2 ? w.z : w.w;
         if constexpr (FP8) {
