@@ -32,6 +32,7 @@
 // the other, at the start of every workgroup, as long as the copy.)
 constexpr int TABLE_WORDS = 928;
 struct InlineTable { uint32_t w[TABLE_WORDS]; };
+struct SmallTable { uint32_t w[112]; };   // of a few requests: a launch of 4 KB of arguments takes the host 1.3 us more
 struct NoTable {};
 
 constexpr int32_t CONTIGUOUS = INT32_MIN;
@@ -56,10 +57,10 @@ static_assert(sizeof(FewReq) == 4 * REQ_WORDS, "REQ_WORDS");
 __host__ __device__ inline int table_units_at(int n_req) { return (n_req + 3) & ~3; }
 __host__ __device__ inline int table_reqs_at(int n_req) { return 2 * table_units_at(n_req); }
 
-template <bool INLINE, class Tab>
+template <class Tab>
 RS_DEVICE const uint32_t* table_of(const Tab& tab, const uint32_t* device_table) {
-    if constexpr (INLINE) return tab.w;
-    else return device_table;
+    if constexpr (std::is_same_v<Tab, NoTable>) return device_table;
+    else return tab.w;
 }
 // The last request whose first item is at most `id`.
 RS_DEVICE int request_of(const uint32_t* table, int n_req, uint32_t id) {
@@ -81,7 +82,7 @@ RS_DEVICE bf16x8 bf16x8_of_codes(uint32_t lo, uint32_t hi) {
     return o;
 }
 struct FewArgs {
-    const uint32_t* table;   // device table (not INLINE)
+    const uint32_t* table;   // device table (NoTable)
     const uint32_t* pages;   // page numbers; null: behind the table's requests
     int n_req, hkv, g;
     const bf16* q;
@@ -172,15 +173,15 @@ struct FewUnit {
 };
 
 constexpr int FEW_ONCE = 2;   // cache policy (nt)
-template <int D, bool FP8, bool LIST, bool INLINE>
-__global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a, std::conditional_t<INLINE, InlineTable, NoTable> tab) {
+template <int D, bool FP8, bool LIST, class Tab>
+__global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a, Tab tab) {
     typedef FewUnit<D, FP8> U;
     constexpr int KS = D / 32, DT = D / 16, NT = U::SUBS, DTU = DT / U::PER;   // sub-tiles of a K unit, feature blocks of a V unit
     // each wavefront's keys and values, in the end all their sums
     constexpr int LDS_BYTES = FEW_WAVES * (2 * U::BYTES > 16 * (D + 4) * 4 ? 2 * U::BYTES : 16 * (D + 4) * 4);
     __shared__ __attribute__((aligned(16))) char lds[LDS_BYTES];
     __shared__ float m_sh[FEW_WAVES][16], l_sh[FEW_WAVES][16];
-    const uint32_t* const table = table_of<INLINE>(tab, a.table);
+    const uint32_t* const table = table_of(tab, a.table);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, c = lane >> 4;
 
@@ -502,11 +503,11 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
 
 // Joins the parts of 16 rows:  M = max_p m_p,  out = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p.  One workgroup per 16 rows and 32
 // features, a quarter of the parts per 64 threads (16 rows x 4 chunks of 8 features).
-template <int D, bool LIST, bool INLINE>
-__global__ __launch_bounds__(256) void few_merge_kernel(FewArgs a, std::conditional_t<INLINE, InlineTable, NoTable> tab) {
+template <int D, bool LIST, class Tab>
+__global__ __launch_bounds__(256) void few_merge_kernel(FewArgs a, Tab tab) {
     __shared__ float m_sh[4][16];
     __shared__ float red[4][64][9];
-    const uint32_t* const table = table_of<INLINE>(tab, a.table);
+    const uint32_t* const table = table_of(tab, a.table);
     FewRows<LIST> rows;
     rows.g = a.g;
     int req, parts, unit, b = 0;

@@ -39,8 +39,8 @@ struct BoundsReq {          // 64 bytes: a FewReq with the bounds' memory in it
 };
 static_assert(sizeof(BoundsReq) == 64, "sixteen words");
 
-template <int D, bool FP8>
-__global__ __launch_bounds__(256) void key_bounds_kernel(int n_req, int hkv, int items, InlineTable tab) {
+template <int D, bool FP8, class Tab>
+__global__ __launch_bounds__(256) void key_bounds_kernel(int n_req, int hkv, int items, Tab tab) {
     constexpr int F = FP8 ? 16 : 8, CH = D / F, STEP = 64 / CH, N = 64 / STEP;   // features of a lane, lanes per key, keys per load, loads
     const uint32_t* const table = tab.w;
     const int lane = threadIdx.x & 63, id = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -215,8 +215,8 @@ RS_DEVICE uint32_t cut_of_keys(const uint32_t* key, int lo, int hi, int take, Se
 constexpr int SELECT_U = 4;                            // groups of 16 blocks that a wavefront has in flight
 constexpr int SELECT_ROUND = 4 * 16 * SELECT_U;        // blocks that a workgroup scores at a time
 enum SelectSteps { SELECT_ALL = 0, SELECT_SCORES = 1, SELECT_FROM_SCORES = 2 };
-template <int D, bool WIDE, int STEPS>
-__global__ __launch_bounds__(STEPS == SELECT_FROM_SCORES ? 1024 : 256) void block_select_kernel(SelectArgs a, InlineTable tab) {
+template <int D, bool WIDE, int STEPS, class Tab>
+__global__ __launch_bounds__(STEPS == SELECT_FROM_SCORES ? 1024 : 256) void block_select_kernel(SelectArgs a, Tab tab) {
     static_assert(WIDE || STEPS == SELECT_ALL, "only few tokens take two launches");
     constexpr int WAVES = STEPS == SELECT_FROM_SCORES ? 16 : 4, TEAM = WIDE ? WAVES : 1, TEAMS = WAVES / TEAM, KK = 2 * D / 64, U = SELECT_U;
     extern __shared__ __attribute__((aligned(16))) uint32_t keys[];   // [tokens][blocks]

@@ -75,7 +75,6 @@ RS_DEVICE void turn_pairs(int j, int rd, const float2* cs, bf16x8& x, bf16x8& y)
 }
 
 constexpr int APPEND_FEW = 8;   // up to this many tokens of a block the values are stored one by one
-struct SmallTable { uint32_t w[112]; };   // the table of a few requests: a launch of 4 KB of arguments takes the host 1.3 us more
 template <int D, bool FP8, bool INTERLEAVED, class Tab>
 __global__ __launch_bounds__(256) void rope_append_kernel(AppendArgs a, Tab tab) {
     constexpr int TASKS = D / 16, EL = FP8 ? 1 : 2;

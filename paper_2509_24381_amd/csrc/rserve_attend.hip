@@ -124,6 +124,17 @@ void for_kind(const rs_ctx* c, bool fp8, F&& f) {
         else f(std::integral_constant<int, 64>{}, std::false_type{});
     }
 }
+// f with the first `words` of the table, in the kernel arguments that hold them.
+template <typename F>
+void with_table(const InlineTable& tab, size_t words, F f) {
+    if (words > sizeof(SmallTable) / 4) {
+        f(tab);
+        return;
+    }
+    SmallTable small;
+    memcpy(small.w, tab.w, words * 4);
+    f(small);
+}
 // ---------------------------------------------------------------- bounds
 rs_status check_bounds(const rs_kv* kv, int layer, int i) {
     if (!kv->bound_codes) return fail(RS_ESTATE, "kvs[%d] has no memory for bounds (rs_kv_attach_bounds)", i);
@@ -182,8 +193,11 @@ rs_status launch_bounds(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* fi
             memcpy(&tab.w[table_reqs_at(n) + 16 * j], &q, sizeof(q));
             items += (uint32_t)(parts[j].b1 - parts[j].b0) * hkv;
         }
-        for_kind(ctx, kvs[0]->fp8, [&](auto d, auto fp8) {
-            hipLaunchKernelGGL((key_bounds_kernel<decltype(d)::value, decltype(fp8)::value>), dim3((items + 3) / 4), dim3(256), 0, st, n, hkv, (int)items, tab);
+        with_table(tab, (size_t)page_at, [&](const auto& table) {
+            for_kind(ctx, kvs[0]->fp8, [&](auto d, auto fp8) {
+                hipLaunchKernelGGL((key_bounds_kernel<decltype(d)::value, decltype(fp8)::value, std::decay_t<decltype(table)>>), dim3((items + 3) / 4), dim3(256), 0,
+                                   st, n, hkv, (int)items, table);
+            });
         });
         RS_HIP(hipGetLastError());
     }
@@ -308,21 +322,12 @@ size_t few_table_pages(rs_kv* const* kvs, const std::vector<FewRequest>& reqs) {
     return n;
 }
 
-template <bool LIST>
-rs_status launch_few(const rs_ctx* ctx, bool fp8, const FewArgs& a, uint32_t items, uint32_t units, bool split, const InlineTable* tab, hipStream_t st) {
+template <bool LIST, class Tab>
+rs_status launch_few(const rs_ctx* ctx, bool fp8, const FewArgs& a, uint32_t items, uint32_t units, bool split, const Tab& tab, hipStream_t st) {
     for_kind(ctx, fp8, [&](auto d, auto f8) {
         constexpr int D = decltype(d)::value;
-        constexpr bool FP8 = decltype(f8)::value;
-        if constexpr (LIST) {
-            hipLaunchKernelGGL((attend_few_kernel<D, FP8, true, false>), dim3(items), dim3(64 * FEW_WAVES), 0, st, a, NoTable{});
-            if (split) hipLaunchKernelGGL((few_merge_kernel<D, true, false>), dim3(units, D / 32), dim3(256), 0, st, a, NoTable{});
-        } else if (tab) {
-            hipLaunchKernelGGL((attend_few_kernel<D, FP8, false, true>), dim3(items), dim3(64 * FEW_WAVES), 0, st, a, *tab);
-            if (split) hipLaunchKernelGGL((few_merge_kernel<D, false, true>), dim3(units, D / 32), dim3(256), 0, st, a, *tab);
-        } else {
-            hipLaunchKernelGGL((attend_few_kernel<D, FP8, false, false>), dim3(items), dim3(64 * FEW_WAVES), 0, st, a, NoTable{});
-            if (split) hipLaunchKernelGGL((few_merge_kernel<D, false, false>), dim3(units, D / 32), dim3(256), 0, st, a, NoTable{});
-        }
+        hipLaunchKernelGGL((attend_few_kernel<D, decltype(f8)::value, LIST, Tab>), dim3(items), dim3(64 * FEW_WAVES), 0, st, a, tab);
+        if (split) hipLaunchKernelGGL((few_merge_kernel<D, LIST, Tab>), dim3(units, D / 32), dim3(256), 0, st, a, tab);
     });
     RS_HIP(hipGetLastError());
     return RS_OK;
@@ -573,7 +578,7 @@ rs_status rs_kv_append(rs_ctx* ctx, const rs_rotary* rotary, int layer, rs_kv* c
             a.positions = at - r0;
         }
         const dim3 grid((unsigned)(i1 - i0), a.hkv + a.q_slices);
-        const auto launch = [&](const auto& table) {
+        with_table(tab, (size_t)words, [&](const auto& table) {
             typedef std::decay_t<decltype(table)> Tab;
             for_kind(ctx, fp8, [&](auto d, auto f8) {
                 if (rotary && rotary->cfg.layout == RS_ROTARY_INTERLEAVED)
@@ -581,14 +586,7 @@ rs_status rs_kv_append(rs_ctx* ctx, const rs_rotary* rotary, int layer, rs_kv* c
                 else
                     hipLaunchKernelGGL((rope_append_kernel<decltype(d)::value, decltype(f8)::value, false, Tab>), grid, dim3(256), 0, st, a, table);
             });
-        };
-        if ((size_t)words <= sizeof(SmallTable) / 4) {
-            SmallTable small;
-            memcpy(small.w, tab.w, (size_t)words * 4);
-            launch(small);
-        } else {
-            launch(tab);
-        }
+        });
         RS_HIP(hipGetLastError());
         i0 = i1;
     }
@@ -649,7 +647,7 @@ rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, 
     FewTable ft;
     InlineTable tab;
     enum { NOTHING, PAGES, ALL } few_staged = NOTHING;   // of the table (see TABLE_WORDS)
-    size_t few_words = 0, few_bytes = 0;   // few_bytes: of the keys and values they read
+    size_t few_words = 0, few_pages = 0, few_bytes = 0;   // few_bytes: of the keys and values they read
     if (!few.empty()) {
         for (const FewRequest& r : few) few_bytes += (size_t)r.tiles * 128 * ctx->kv_dim * (fp8 ? 1 : 2);
         for (FewRequest& r : few) r.once = few_bytes >= FEW_ONCE_BYTES && r.row_blocks == 1;
@@ -660,8 +658,8 @@ rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, 
         a.scale_log2e = scale_log2e;
         a.slots = reinterpret_cast<float*>(ws + L.slots_at);
         few_words = few_table_words(few);
-        const size_t pages = few_table_pages(kvs, few);
-        few_staged = few_words + pages <= TABLE_WORDS ? NOTHING : few_words <= TABLE_WORDS ? PAGES : ALL;
+        few_pages = few_table_pages(kvs, few);
+        few_staged = few_words + few_pages <= TABLE_WORDS ? NOTHING : few_words <= TABLE_WORDS ? PAGES : ALL;
         if (few_staged == NOTHING) ft = write_few_table(ctx, layer, kvs, few, false, tab.w, tab.w + few_words);
     }
     const bool staged = chunks || few_staged != NOTHING;
@@ -672,11 +670,11 @@ rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, 
     if (few_staged == ALL) {
         ft = write_few_table(ctx, layer, kvs, few, false, reinterpret_cast<uint32_t*>(stage), reinterpret_cast<uint32_t*>(stage) + few_words);
         a.table = reinterpret_cast<const uint32_t*>(ws);
-        staged_bytes = align_up((few_words + few_table_pages(kvs, few)) * 4, 16);
+        staged_bytes = align_up((few_words + few_pages) * 4, 16);
     } else if (few_staged == PAGES) {
         ft = write_few_table(ctx, layer, kvs, few, false, tab.w, reinterpret_cast<uint32_t*>(stage));
         a.pages = reinterpret_cast<const uint32_t*>(ctx->pinned_dev[slot]);
-        staged_bytes = align_up(few_table_pages(kvs, few) * 4, 16);
+        staged_bytes = align_up(few_pages * 4, 16);
     }
     // ---- chunks
     std::vector<ReqDesc> reqs;
@@ -740,9 +738,12 @@ rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, 
         RS_HIP(hipGetLastError());
         if (a.pages) a.pages = reinterpret_cast<const uint32_t*>(ws);   // (copied too)
     }
-    if (!few.empty() &&
-        (s = launch_few<false>(ctx, fp8, a, ft.items, ft.units, ft.any_split, few_staged == ALL ? nullptr : &tab, st)) != RS_OK)
-        return s;
+    if (!few.empty()) {
+        const auto launch = [&](const auto& table) { s = launch_few<false>(ctx, fp8, a, ft.items, ft.units, ft.any_split, table, st); };
+        if (few_staged == ALL) launch(NoTable{});
+        else with_table(tab, few_words + (few_staged == NOTHING ? few_pages : 0), launch);
+        if (s != RS_OK) return s;
+    }
     if (staged && (s = ring_commit(ctx, st)) != RS_OK) return s;
     if (!chunks) return RS_OK;
     const ReqDesc* const d_reqs = reinterpret_cast<const ReqDesc*>(ws + at_reqs);
@@ -828,10 +829,19 @@ rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int*
     char* const ws = reinterpret_cast<char*>(workspace);
     const bool fp8 = kvs[0]->fp8;
     if (!ctx->select_ready) {   // first use on this context: opt in to the LDS size once
-        for (const void* k : {(const void*)block_select_kernel<64, false, SELECT_ALL>, (const void*)block_select_kernel<64, true, SELECT_ALL>,
-                              (const void*)block_select_kernel<64, true, SELECT_FROM_SCORES>, (const void*)block_select_kernel<128, false, SELECT_ALL>,
-                              (const void*)block_select_kernel<128, true, SELECT_ALL>, (const void*)block_select_kernel<128, true, SELECT_FROM_SCORES>})
-            RS_HIP(hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)SELECT_LDS));
+        const auto opt_in = [](auto d, auto table) -> rs_status {
+            constexpr int D = decltype(d)::value;
+            typedef decltype(table) Tab;
+            for (const void* k : {(const void*)block_select_kernel<D, false, SELECT_ALL, Tab>, (const void*)block_select_kernel<D, true, SELECT_ALL, Tab>,
+                                  (const void*)block_select_kernel<D, true, SELECT_FROM_SCORES, Tab>})
+                RS_HIP(hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)SELECT_LDS));
+            return RS_OK;
+        };
+        const std::integral_constant<int, 64> narrow{};
+        const std::integral_constant<int, 128> broad{};
+        if ((s = opt_in(narrow, InlineTable{})) != RS_OK || (s = opt_in(narrow, SmallTable{})) != RS_OK || (s = opt_in(broad, InlineTable{})) != RS_OK ||
+            (s = opt_in(broad, SmallTable{})) != RS_OK)
+            return s;
         ctx->select_ready = true;
     }
     // bounds that are missing
@@ -905,15 +915,18 @@ rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int*
         const size_t lds = (size_t)sa.tokens * sa.blocks * 4;
         const auto select = [&](auto d) {
             constexpr int D = decltype(d)::value;
-            if (sa.split > 1) {
-                sa.groups = (int)groups * sa.split;
-                hipLaunchKernelGGL((block_select_kernel<D, true, SELECT_SCORES>), dim3(groups * sa.split + copying, f.n_kv_heads), dim3(threads), 0, st, sa, tab);
-                hipLaunchKernelGGL((block_select_kernel<D, true, SELECT_FROM_SCORES>), dim3(groups, f.n_kv_heads), dim3(1024), lds, st, sa, tab);
-                return;
-            }
-            sa.groups = (int)groups;
-            if (wide) hipLaunchKernelGGL((block_select_kernel<D, true, SELECT_ALL>), dim3(groups + copying, f.n_kv_heads), dim3(threads), lds, st, sa, tab);
-            else hipLaunchKernelGGL((block_select_kernel<D, false, SELECT_ALL>), dim3(groups + copying, f.n_kv_heads), dim3(threads), lds, st, sa, tab);
+            with_table(tab, (size_t)table_reqs_at(n) + 16 * n, [&](const auto& table) {
+                typedef std::decay_t<decltype(table)> Tab;
+                if (sa.split > 1) {
+                    sa.groups = (int)groups * sa.split;
+                    hipLaunchKernelGGL((block_select_kernel<D, true, SELECT_SCORES, Tab>), dim3(groups * sa.split + copying, f.n_kv_heads), dim3(threads), 0, st, sa, table);
+                    hipLaunchKernelGGL((block_select_kernel<D, true, SELECT_FROM_SCORES, Tab>), dim3(groups, f.n_kv_heads), dim3(1024), lds, st, sa, table);
+                    return;
+                }
+                sa.groups = (int)groups;
+                if (wide) hipLaunchKernelGGL((block_select_kernel<D, true, SELECT_ALL, Tab>), dim3(groups + copying, f.n_kv_heads), dim3(threads), lds, st, sa, table);
+                else hipLaunchKernelGGL((block_select_kernel<D, false, SELECT_ALL, Tab>), dim3(groups + copying, f.n_kv_heads), dim3(threads), lds, st, sa, table);
+            });
         };
         if (f.head_dim == 128) select(std::integral_constant<int, 128>{});
         else select(std::integral_constant<int, 64>{});
@@ -930,7 +943,7 @@ rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int*
     a.chosen = list;
     a.n_blocks = n_blocks;
     a.list_parts = parts;
-    return launch_few<true>(ctx, fp8, a, (uint32_t)(units * parts), (uint32_t)(units * rbn), parts > 1, nullptr, st);
+    return launch_few<true>(ctx, fp8, a, (uint32_t)(units * parts), (uint32_t)(units * rbn), parts > 1, NoTable{}, st);
 } catch (const std::exception& e) {
     return not_allocated(e);
 }
