@@ -26,6 +26,8 @@ RS_DEVICE float limited(float x) { return x == x ? fminf(fmaxf(x, -BOUND_LIMIT),
 // One wavefront per (block, KV head), bound by reading K once: all of a tile's loads are in flight together, a lane holding 8 (8-bit: 16)
 // features of a sixteenth (an eighth) of the keys.  Maxima and minima do not depend on the order they are taken in, and
 // codes are whole numbers: the result is the same bits whatever computes it.
+//   e the least exponent with max |k| <= 127 2^e (limited to 2^100, NaN as 0),  high = ceil(max_key k / 2^e),  low = floor(min_key k / 2^e)
+// Measured: 512 blocks of 4 KV heads, 34 MB, 9.6 us (3.5 TB/s; 3 us of it before the first bytes arrive); 32 blocks 5.8 us.
 struct BoundsReq {          // 64 bytes: a FewReq with the bounds' memory in it
     uint64_t k;
     uint64_t head_bytes;
@@ -103,12 +105,15 @@ __global__ __launch_bounds__(256) void key_bounds_kernel(int n_req, int hkv, int
 //  1. every token's p and n (see the score in the header), int8, into LDS;
 //  2. scores of 16 blocks x 4 tokens (of 16 it has room for) per v_mfma_i32_16x16x64_i8 chain (the contraction runs over high and low codes), as keys
 //     that order like the scores, into LDS;
+//     score[block] = unit sum_d (p_d high_d - n_d low_d),  p and n the heads' positive and negative codes, summed: whole numbers, one product
 //  3. a team per token finds the score that the last selected block has, digit by digit of the keys' range (a histogram in LDS per
 //     digit: integers, in any order the same), and writes the blocks down in ascending order.
 // With many tokens a workgroup has four, a wavefront each, and takes all three steps.  With few (WIDE) it has one, and where that has more
 // blocks than a workgroup scores at once, the first two steps are a launch of their own, of a workgroup per 256 blocks: a compute unit alone
 // gets 33 bytes per ns, 16 us for the bounds of 2046 blocks.  (One launch, the last workgroup to finish selecting: the fence that makes
 // keys visible across the chip takes longer than a second launch, 7 us.)
+// Measured: one token on 2046 blocks 6.0 and 6.2 us, 256 tokens on 250 blocks 10.6: chains from queries to codes, scores, digits, list.  (Reductions
+// over lanes stay in registers; through LDS the three took 7.3, 7.5 and 12.4.)
 struct SelectReq {          // 64 bytes
     uint64_t codes, units;
     int32_t room;

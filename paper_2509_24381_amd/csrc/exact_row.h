@@ -10,7 +10,7 @@ RS_DEVICE float tile_element(global_bytes tile, int i) {
     else return bf16_to_f32(*reinterpret_cast<const __attribute__((address_space(1))) bf16*>(tile + 2 * (size_t)i));
 }
 
-// One query row over tiles [i0, i1), by one wavefront, without the matrix pipe: what the kernels below fall back on where a row's result is
+// One query row over tiles [i0, i1), by one wavefront, without the matrix pipe: what the attention kernels fall back on where a row's result is
 // not finite.  A masked value enters their products with weight zero, and zero times an infinity or NaN is NaN; here it does not enter.
 // Returns the reference and row sum, and in o the unnormalised output of features lane + 64 i.
 template <int D, bool FP8, class TileAt>

@@ -5,6 +5,12 @@
 // in one 64-token block, either of one KV head (keys row by row; values turned through LDS, 8 tokens per store, when there are many) or
 // of a share of the query heads.  A task is 16 features of a head whose pairs are complete in it: two 16-byte loads, 64 bytes of cosines
 // and sines, two 16-byte stores.
+//
+//   (a, b) -> (a cos - b sin, b cos + a sin), in fp32 from fp32 cosines and sines of 64-bit angles, rounded to bfloat16 once; 8-bit caches
+//   take the rounded key's code, so that they hold what a bfloat16 cache's content would be encoded as.
+//
+// Measured (28 query heads, 4 KV heads, d = 128), us of the kernel: one token 3 to 4.2, 64 single tokens 5.1, 2048 rows of 8 requests into 8-bit
+// pages, 36 MB, 10.6 (3.4 TB/s).  With four tasks of a thread's queries loaded together as well: 11 to 12 (registers).
 #pragma once
 #include "attend_few.h"
 #include "common.h"

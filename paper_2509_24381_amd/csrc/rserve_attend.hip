@@ -44,9 +44,12 @@ constexpr long FEW_TILES = 2000, FEW_TILES_BESIDE = 4500, FEW_TILES_FP8 = 6000;
 // before.  us with / without it, behind a fill of 1 GB: 8 MB 14.6 / 15.6, 35 MB 19.6 / 26.6, 141 MB 38.3 / 69.5; call after call on the
 // same caches: 4 MB 15.7 / 14.6, 8 MB 20.2 / 20.4, 141 MB 53.3 / 54.5.
 constexpr size_t FEW_ONCE_BYTES = (size_t)8 << 20;
-constexpr int FEW_PLACES = 2;      // workgroups of attend_few_kernel that a compute unit holds
+// Workgroups per compute unit that parts are made for.  Four fit, but two stream as fast as four.  us a pass with 1 / 2 / 3 / 4: 64 requests on up to
+// 8000 86.0 / 89.4 / 87.1 / 86.1, 16 on up to 32000, 8 bits, 65.1 / 60.2 / 60.9 / 62.3, 24 of 3 and one of 12 81.6 / 53.7 / 57.4 / 57.7.
+constexpr int FEW_PLACES = 2;
 constexpr size_t SLOT_ROWS = 65536;   // rows there is room for in the slots of split key ranges
-// Tokens times KV heads up to which workgroups share a token's blocks (block_select_kernel).
+// Tokens times KV heads up to which a workgroup selects for one token, and several share its blocks; beyond, for four.  us a pass, four / one, 4 KV
+// heads: 16 tokens on 8000 20.2 / 19.3, on 60000 34.7 / 27.3; 64 on 16000 29.2 / 28.7, on 60000 42.1 / 40.4; 96 on 16000 34.8 / 35.5; 128 on 60000 47.6 / 51.7.
 constexpr size_t SELECT_WIDE_UNITS = 256;
 constexpr size_t SELECT_LDS = (size_t)SELECT_MAX_BLOCKS * 4;
 
@@ -236,9 +239,9 @@ size_t expansion_bytes(const rs_ctx* c, long tokens) { return (size_t)2 * align_
 // faster they stream: a tile then takes 0.66 of one.  With more, the last ones start late: a share of the longest comes on top.  Where two or
 // all four wavefronts need every tile (16 rows each) it takes 2 and 3 times as long, and parts are that much shorter (us a pass, all
 // alike -> so: 30 single tokens on up to 8000 beside 4 requests of 5 on 3000, 64 query heads, 8 KV heads, 142.7 -> 115.5, 8 bits
-// 91.3 -> 55.8; 24 requests of 3 on up to 6000 beside one of 12 on 5000 68.4 -> 53.4; one of 4 on 8000, alone, 15.8 -> 17.2).  us a pass, parts of 4 / 8 / 16 / 24 / 48 tiles: 64 requests on up to 8000 tokens
-// 100.5 / 93.8 / 88.7 / 92.2 / 90.1; 16 on up to 32000, 8 bits, 82.8 / 77.6 / 70.6 / 67.6 / 61.1; 24 of 3 tokens on up to 6000, 8 query
-// heads per KV head, 77.5 / 73.2 / 72.4 / 87.2 / 99.7.
+// 91.3 -> 55.8; 24 requests of 3 on up to 6000 beside one of 12 on 5000 68.4 -> 53.4; one of 4 on 8000, alone, 15.8 -> 17.2).
+// us a pass, parts of 4 / 8 / 16 / 24 / 48 tiles, and with this estimate's: 64 requests on up to 8000 tokens 97.4 / 93.2 / 86.0 / 86.6 / 89.0, 88.3; 16 on up to 32000, 8 bits,
+// 73.2 / 68.6 / 66.1 / 64.6 / 59.4, 60.2; 24 of 3 tokens on up to 6000 and one of 12, 64 and 8 heads, 79.6 / 69.5 / 58.3 / 56.6 / 67.0, 54.3.
 struct FewRequest {
     int kv, row0, T;       // index into kvs, first row, rows
     int units, tiles;      // items per part, tiles
@@ -865,11 +868,18 @@ rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int*
         row += lens[i];
     }
     const int rbn = few_row_blocks(ctx->group), units = (int)rows * f.n_kv_heads;
+    // Parts of a list: a block per wavefront where there are places for that, else a power of two, so that wavefronts' shares stay even; one part
+    // where a list is short or three quarters of the compute units are busy without.  us a pass with 1 / 2 / 4 / 8 parts, 4 KV heads: lists of 16,
+    // one token 17.5 / 18.4 / 17.5 / 17.2, 32 tokens 18.9 / 20.5 / 20.5 / 22.5; of 32, one 21.7 / 20.3 / 18.4 / 17.4, 16 24.2 / 21.1 / 19.5 / 20.1,
+    // 32 25.0 / 22.5 / 22.4 / 24.9, 48 25.2 / 26.0 / 26.5 / 30.4, 64 26.9 / 28.9 / 31.0 / 35.8; of 64, 8 36.5 / 25.9 / 22.2 / 20.0, 48 35.4 / 33.9 / 33.2 / 36.4.
+    // Lists of 48, one token: 12 parts 17.5, 8 parts 18.4; 24 tokens (96 units): 6 parts 26.3, 4 parts 24.4.
     int parts = 1;
-    const int places = FEW_PLACES * ctx->n_cu;
-    if (units < places) parts = std::min((std::min(n_blocks, longest) + FEW_WAVES - 1) / FEW_WAVES, (places + units - 1) / units);
-    while (parts > 1 && (size_t)units * parts * rbn > SLOT_ROWS / 16) --parts;
-    parts = std::max(1, std::min(parts, FEW_MAX_PARTS));
+    const int held = std::min(n_blocks, longest), places = FEW_PLACES * ctx->n_cu, apart = std::min((held + FEW_WAVES - 1) / FEW_WAVES, FEW_MAX_PARTS);
+    if (held > 4 * FEW_WAVES && 4 * units <= 3 * ctx->n_cu) {
+        if (apart * units <= places) parts = apart;
+        else while (2 * parts * units <= places && 2 * parts <= apart) parts *= 2;
+    }
+    if ((size_t)units * parts * rbn > SLOT_ROWS / 16) parts = 1;
     int slot = 0;
     if ((s = ring_acquire(ctx, st, &slot)) != RS_OK) return s;
     uint32_t* const table = reinterpret_cast<uint32_t*>(ctx->pinned[slot]);
