@@ -185,19 +185,21 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else int(t.data_ptr())
 
 
-_raw_stream = None   # handle of a device's current stream, once a GPU has been seen
+_raw_stream = _device = None   # handle of a device's current stream, and the current device, once a GPU has been seen
 
 
 def _stream_handle(stream) -> Optional[int]:
-    global _raw_stream
+    global _raw_stream, _device
     if stream is None:
-        import torch
         if _raw_stream is None:
+            import torch
             if not torch.cuda.is_available():
                 return None  # GPU-less host: the call can only reach the library's argument checks
-            # (the current stream's handle without the object around it, where torch has that: 0.4 us instead of 2.9)
+            # (the current stream's handle without the object around it, where torch has that: 0.2 us instead of 2.9)
+            torch.cuda.current_device()   # (initialises)
+            _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
             _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
-        return _raw_stream(torch.cuda.current_device()) or None
+        return _raw_stream(_device()) or None
     if isinstance(stream, int):
         return stream or None
     return int(stream.cuda_stream) or None
@@ -300,7 +302,7 @@ def _ints(values, n: int, what: str):
     """The address of a C array of at least n whole numbers, or None; the array has to outlive the call."""
     if values is None:
         return None
-    a = int_array(values)
+    a = values if isinstance(values, C.Array) else int_array(values)
     if len(a) < n or a._type_ is not C.c_int:
         raise RsError(-1, f"{what} has {len(a)} entries, the call needs {n} ints")
     return a
@@ -311,10 +313,11 @@ class CacheSet:
 
     def __init__(self, caches: Sequence["KVCache"]):
         self.caches = list(caches)
+        self.n = len(self.caches)
         self.handles = (C.c_void_p * max(len(self.caches), 1))(*[kv.handle.value for kv in self.caches])
 
     def __len__(self):
-        return len(self.caches)
+        return self.n
 
 
 def _cache_set(kvs) -> CacheSet:
@@ -325,20 +328,24 @@ _bf16 = None   # torch.bfloat16, once torch is there
 
 
 def _rows(t, what: str, rows: int, width: int):
-    """(address, distance between rows) of a bf16 tensor [rows, width] or [rows, heads, d] whose rows are contiguous."""
+    """(address, distance between rows) of a bf16 tensor [rows, width] or [rows, heads, d] whose rows are contiguous; rows: the sum of lens."""
     global _bf16
+    shape = t.shape
+    if shape == (rows, width) and t.dtype is _bf16:   # (the common case, in one go)
+        ld, inner = t.stride()
+        if inner == 1:
+            return t.data_ptr(), ld if rows > 1 else width
     if _bf16 is None:
         import torch
         _bf16 = torch.bfloat16
-    shape, stride = t.shape, t.stride()
-    if len(shape) == 2 and stride[1] == 1 and shape[1] == width and shape[0] == rows and t.dtype is _bf16:   # (the common case, in one go)
-        return t.data_ptr(), stride[0] if rows > 1 else width
-    inner = 1
+    if shape and shape[0] != rows:
+        raise RsError(-1, f"lens add up to {rows}, {what} has {shape[0]} rows")
+    stride, inner = t.stride(), 1
     for n, s in zip(reversed(shape[1:]), reversed(stride[1:])):
         if s != inner and n != 1:
             raise RsError(-1, f"the rows of {what} are not contiguous")
         inner *= n
-    if t.dtype is not _bf16 or not shape or shape[0] != rows or inner != width:
+    if t.dtype is not _bf16 or not shape or inner != width:
         raise RsError(-1, f"{what} must be bfloat16 [{rows}, {width}]: {t.dtype} {list(shape)}")
     return t.data_ptr(), stride[0] if rows > 1 else width
 
@@ -504,6 +511,7 @@ class KVCache:
 class Context:
     def __init__(self, cfg: LayerConfig):
         self.cfg = cfg
+        self._q_width, self._kv_width = cfg.n_q_heads * cfg.head_dim, cfg.n_kv_heads * cfg.head_dim
         self.lib = load_library()
         h = C.c_void_p()
         c = cfg._c()
@@ -660,20 +668,17 @@ class Context:
         """Rotates new tokens' queries and keys, and stores keys and values into the caches.  kvs: caches or a CacheSet; lens: new tokens per
         request; q, q_out: bf16 rows of all query heads (both None: none), k, v: of all KV heads, rows possibly strided; starts: first
         cache slots (None: at the end; else later tokens are dropped); positions: rotary positions per row (None: the slots)."""
-        cs, cfg = _cache_set(kvs), self.cfg
-        rows, qw, kw = int(k.shape[0]), cfg.n_q_heads * cfg.head_dim, cfg.n_kv_heads * cfg.head_dim
-        n = _ints(lens, len(cs), "lens")
-        if _sum_of(n, len(cs)) != rows:
-            raise RsError(-1, f"lens add up to {_sum_of(n, len(cs))}, k has {rows} rows")
-        st, ps = _ints(starts, len(cs), "starts"), None
+        cs = _cache_set(kvs)
+        r, n = cs.n, _ints(lens, cs.n, "lens")
+        rows, st, ps = _sum_of(n, r), _ints(starts, r, "starts"), None
+        kp, ldk = _rows(k, "k", rows, self._kv_width)
+        vp, ldv = _rows(v, "v", rows, self._kv_width)
         if positions is not None:
             ps = _ints(positions.tolist() if hasattr(positions, "tolist") else positions, rows, "positions")
-        qp, ldq = _rows(q, "q", rows, qw) if q is not None else (None, 0)
-        op, ldo = _rows(q_out, "q_out", rows, qw) if q_out is not None else (None, 0)
-        kp, ldk = _rows(k, "k", rows, kw)
-        vp, ldv = _rows(v, "v", rows, kw)
-        _check(self.lib.rs_kv_append(self.handle, rotary.handle if rotary is not None else None, layer, cs.handles, st, n, len(cs), ps, qp, ldq, kp, ldk, vp,
-                                     ldv, op, ldo, _stream_handle(stream)))
+        qp, ldq = _rows(q, "q", rows, self._q_width) if q is not None else (None, 0)
+        op, ldo = _rows(q_out, "q_out", rows, self._q_width) if q_out is not None else (None, 0)
+        _check(self.lib.rs_kv_append(self.handle, rotary.handle if rotary is not None else None, layer, cs.handles, st, n, r, ps, qp, ldq, kp, ldk, vp, ldv, op,
+                                     ldo, _stream_handle(stream)))
         return q_out
 
     def attend_workspace(self, max_rows: int, max_requests: int = 1, fp8_visible_tokens: int = 0, n_blocks: int = 0):
@@ -685,38 +690,34 @@ class Context:
 
     def attend(self, layer: int, kvs, lens, q, out, workspace, scale: float = 0.0, stream=None):
         """Attention of every request's last lens[i] cached tokens over its cache; q, out: bf16 rows of all query heads; scale 0: 1/sqrt(d)."""
-        cs, width = _cache_set(kvs), self.cfg.n_q_heads * self.cfg.head_dim
-        rows = int(q.shape[0])
-        n = _ints(lens, len(cs), "lens")
-        if _sum_of(n, len(cs)) != rows:
-            raise RsError(-1, f"lens add up to {_sum_of(n, len(cs))}, q has {rows} rows")
-        qp, ldq = _rows(q, "q", rows, width)
-        op, ldo = _rows(out, "out", rows, width)
-        _check(self.lib.rs_attend(self.handle, layer, cs.handles, n, len(cs), qp, ldq, op, ldo, scale, _ptr(workspace), workspace.numel(),
-                                  _stream_handle(stream)))
+        cs = _cache_set(kvs)
+        r, n = cs.n, _ints(lens, cs.n, "lens")
+        rows = _sum_of(n, r)
+        qp, ldq = _rows(q, "q", rows, self._q_width)
+        op, ldo = _rows(out, "out", rows, self._q_width)
+        _check(self.lib.rs_attend(self.handle, layer, cs.handles, n, r, qp, ldq, op, ldo, scale, workspace.data_ptr(), workspace.numel(), _stream_handle(stream)))
         return out
 
     def bounds_update(self, layer: int, kvs, firsts=None, stream=None):
         """Bounds on the keys of the caches' finished blocks: of those that have none, or of those from slots `firsts` on."""
         cs = _cache_set(kvs)
-        _check(self.lib.rs_kv_bounds_update(self.handle, layer, cs.handles, _ints(firsts, len(cs), "firsts"), len(cs), _stream_handle(stream)))
+        _check(self.lib.rs_kv_bounds_update(self.handle, layer, cs.handles, _ints(firsts, cs.n, "firsts"), cs.n, _stream_handle(stream)))
 
     def attend_blocks(self, layer: int, kvs, lens, q, out, workspace, n_blocks: int, n_first: int = 1, n_last: int = 2, chosen=None,
                       scale: float = 0.0, stream=None):
         """attend over at most n_blocks 64-token blocks per token and KV head: the first n_first, the last n_last, and those with the best
         scores.  chosen: int32 [rows, Hkv, n_blocks] or None, receives them."""
-        import torch
-        cs, cfg = _cache_set(kvs), self.cfg
-        rows, width = int(q.shape[0]), cfg.n_q_heads * cfg.head_dim
-        n = _ints(lens, len(cs), "lens")
-        if _sum_of(n, len(cs)) != rows:
-            raise RsError(-1, f"lens add up to {_sum_of(n, len(cs))}, q has {rows} rows")
-        if chosen is not None and (chosen.dtype is not torch.int32 or not chosen.is_contiguous() or chosen.numel() != rows * cfg.n_kv_heads * n_blocks):
-            raise RsError(-1, f"chosen must be contiguous int32 [{rows}, {cfg.n_kv_heads}, {n_blocks}]: {chosen.dtype} {list(chosen.shape)}")
-        qp, ldq = _rows(q, "q", rows, width)
-        op, ldo = _rows(out, "out", rows, width)
-        _check(self.lib.rs_attend_blocks(self.handle, layer, cs.handles, n, len(cs), qp, ldq, op, ldo, n_blocks, n_first, n_last, scale, _ptr(chosen),
-                                         _ptr(workspace), workspace.numel(), _stream_handle(stream)))
+        cs = _cache_set(kvs)
+        r, n = cs.n, _ints(lens, cs.n, "lens")
+        rows = _sum_of(n, r)
+        qp, ldq = _rows(q, "q", rows, self._q_width)
+        op, ldo = _rows(out, "out", rows, self._q_width)
+        if chosen is not None:
+            import torch
+            if chosen.dtype is not torch.int32 or not chosen.is_contiguous() or chosen.numel() != rows * self.cfg.n_kv_heads * n_blocks:
+                raise RsError(-1, f"chosen must be contiguous int32 [{rows}, {self.cfg.n_kv_heads}, {n_blocks}]: {chosen.dtype} {list(chosen.shape)}")
+        _check(self.lib.rs_attend_blocks(self.handle, layer, cs.handles, n, r, qp, ldq, op, ldo, n_blocks, n_first, n_last, scale, _ptr(chosen),
+                                         workspace.data_ptr(), workspace.numel(), _stream_handle(stream)))
         return out
 
 
