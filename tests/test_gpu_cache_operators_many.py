@@ -1,0 +1,136 @@
+"""GPU: the operators on caches with more requests, pages and blocks than one form of their descriptors holds, and lists of blocks that are
+cut into parts, against the 64-bit oracle; tolerances as in test_gpu_cache_operators.py."""
+import numpy as np
+import pytest
+import torch
+
+import test_gpu_cache_operators as T
+from oracle import cache_ops as O
+
+pytestmark = pytest.mark.gpu
+
+
+def filled(ctx, kind, held, seed, d=64, hkv=2):
+    g = T.gen(seed)
+    kvs = T.caches(ctx, kind, held)
+    content = [(T.normal(g, n, hkv, d), T.normal(g, n, hkv, d)) for n in held]
+    T.fill(kvs, content)
+    return kvs, content, g
+
+
+def check_attend(ctx, kind, kvs, content, held, lens, g):
+    hq, hkv, d = ctx.cfg.n_q_heads, ctx.cfg.n_kv_heads, ctx.cfg.head_dim
+    rows = sum(lens)
+    q = T.normal(g, rows, hq * d, std=1.5)
+    out = torch.full_like(q, float("nan"))
+    ctx.attend(0, kvs, lens, q, out, ctx.attend_workspace(rows, len(held), fp8_visible_tokens=sum(held)))
+    at = 0
+    for n, t, (k, v) in zip(held, lens, content):
+        if t:
+            ref, mag = O.attend(T.f64(q[at: at + t]).reshape(t, hq, d), T.stored(k, kind, T.K_SCALE), T.stored(v, kind, T.V_SCALE), n - t)
+            T.assert_attention(out[at: at + t], ref, mag, f"{n} cached, {t} rows")
+        at += t
+
+
+@pytest.mark.parametrize("kind", ["paged", "paged_fp8"])
+@pytest.mark.parametrize("requests, longest", [(66, 60), (67, 60), (100, 40), (128, 700), (20, 3500)])
+@pytest.mark.parametrize("chunk", [0, 60])
+def test_attend_of_many_requests_and_pages(kind, requests, longest, chunk, monkeypatch):
+    """Descriptors in the kernel arguments, page numbers beside them or in place, all of it in the workspace; with a chunk for the chunk
+    kernel beside them, whose own descriptors are copied in the same launch."""
+    monkeypatch.setenv("RS_ATTEND_FEW", "0")
+    ctx = T.context(4, 2, 64, max_requests=160)
+    held = [1 + (i * 37 + longest) % longest for i in range(requests)] + ([chunk + 130] if chunk else [])
+    lens = [0 if i == 3 else 2 if n > 1 and i % 5 == 0 else 1 for i, n in enumerate(held)]
+    if chunk:
+        lens[-1] = chunk
+    kvs, content, g = filled(ctx, kind, held, 60)
+    check_attend(ctx, kind, kvs, content, held, lens, g)
+
+
+@pytest.mark.parametrize("kind", T.KINDS)
+def test_append_of_many_requests(kind):
+    """A token for every one of 90 requests, with explicit positions: more than one launch's descriptors."""
+    ctx = T.context(4, 2, 64, max_requests=160)
+    held = [(i * 29) % 130 for i in range(90)]
+    g = T.gen(61)
+    kvs = T.caches(ctx, kind, [n + 1 for n in held])
+    content = [(T.normal(g, n, 2, 64), T.normal(g, n, 2, 64)) for n in held]
+    for kv, (k, v) in zip(kvs, content):
+        if len(k):
+            kv.import_(0, k, v)
+    form = T.ROTARY_FORMS[1]
+    rot = T.rotary_of(ctx, 32, form)
+    pos = [(7 * i) % 2000 for i in range(90)]
+    q, k, v = T.normal(g, 90, 256), T.normal(g, 90, 128), T.normal(g, 90, 128)
+    out = torch.empty_like(q)
+    ctx.kv_append(0, kvs, [1] * 90, q, k, v, out, rotary=rot, positions=pos)
+    ref = T.rotated(q.view(90, 4, 64), np.array(pos), 32, form)
+    assert (np.abs(T.f64(out).reshape(ref.shape) - ref) <= T.rotation_bound(q.view(90, 4, 64), ref, 32, form)).all()
+    assert [kv.length(0) for kv in kvs] == [n + 1 for n in held]
+    for i, (kv, n) in enumerate(zip(kvs, held)):
+        _, ve = kv.export(0)
+        assert np.array_equal(T.f64(ve[n]), T.stored(v[i].view(2, 64), kind, T.V_SCALE))
+
+
+@pytest.mark.parametrize("kind", ["paged", "paged_fp8"])
+def test_bounds_of_more_pages_than_one_launch_describes(kind):
+    ctx = T.context(4, 2, 64, max_requests=160)
+    held = [64 * (i % 60) + 5 * i for i in range(50)]
+    kvs, content, _ = filled(ctx, kind, [max(n, 1) for n in held], 62)
+    memory = [kv.new_bounds(64 * 64) for kv in kvs]
+    ctx.bounds_update(0, kvs)
+    for kv, (k, _), (codes, units) in zip(kvs, content, memory):
+        want_codes, want_units = T.bounds_of(T.stored(k, kind, T.K_SCALE))
+        full = len(want_codes)
+        assert kv.bounded(0) == full == len(k) // 64
+        assert np.array_equal(codes[0, :, :full].cpu().numpy().transpose(1, 0, 2, 3), want_codes)
+        assert np.array_equal(T.f64(units[0, :, :full]).T, want_units)
+
+
+@pytest.mark.parametrize("rows", [1, 3])
+def test_blocks_of_many_requests(rows):
+    """100 requests: more descriptors than one selection launch has, pages beyond the kernel arguments, bounds that are missing."""
+    ctx = T.context(4, 2, 64, max_requests=160)
+    held = [rows + (i * 91) % 900 for i in range(100)]
+    lens = [0 if i % 9 == 4 else rows for i in range(100)]
+    kvs, content, g = filled(ctx, "paged", held, 63)
+    for kv, n in zip(kvs, held):
+        kv.new_bounds(n + 64)
+    q = T.normal(g, sum(lens), 256, std=1.5)
+    out, chosen = T.run_blocks(ctx, kvs, lens, q, 5, 1, 2)
+    T.check_blocks(ctx, "paged", held, lens, content, q, out, chosen, 5, 1, 2)
+
+
+@pytest.mark.parametrize("kind", ["contiguous", "paged_fp8"])
+@pytest.mark.parametrize("hq, hkv, d", [(14, 2, 128), (40, 1, 64)])
+@pytest.mark.parametrize("held, lens, n_blocks", [([4500], [1], 48), ([2500, 4000, 600], [1, 3, 2], 33), ([3000], [70], 20), ([1700], [100], 17), ([1100], [200], 16)])
+def test_lists_in_parts(kind, hq, hkv, d, held, lens, n_blocks):
+    """Lists of more blocks than four wavefronts take alone are cut into parts by how many rows there are; shorter ones are not."""
+    ctx = T.context(hq, hkv, d)
+    kvs, content, g = filled(ctx, kind, held, 64, d, hkv)
+    for kv, n in zip(kvs, held):
+        kv.new_bounds(n + 64)
+    q = T.normal(g, sum(lens), hq * d, std=1.5)
+    out, chosen = T.run_blocks(ctx, kvs, lens, q, n_blocks, 1, 2)
+    T.check_blocks(ctx, kind, held, lens, content, q, out, chosen, n_blocks, 1, 2)
+
+
+def test_masked_values_that_are_not_finite_in_lists_in_parts():
+    """What lies behind a row's own slot, in the block it is in, is infinite or NaN; lists in parts, and slots of rows that end in another part."""
+    hq, hkv, d = 14, 2, 128
+    ctx = T.context(hq, hkv, d)
+    g = T.gen(65)
+    n, rows = 64 * 40, 30
+    k, v = T.normal(g, n, hkv, d), T.normal(g, n, hkv, d)
+    kv, = T.caches(ctx, "paged", [n])
+    dirty_k, dirty_v = k.clone(), v.clone()
+    dirty_v[-4:, 0] = float("nan")
+    dirty_k[-4:, 1] = float("inf")
+    dirty_v[-8:-4, 1, :5] = float("-inf")
+    kv.import_(0, dirty_k, dirty_v)
+    kv.new_bounds(n)
+    q = T.normal(g, rows, hq * d)
+    out, chosen = T.run_blocks(ctx, [kv], [rows], q, 40, 1, 2)
+    ref, mag = O.attend(T.f64(q).reshape(rows, hq, d), T.f64(k), T.f64(v), n - rows)
+    T.assert_attention(out[:rows - 8], ref[:rows - 8], mag[:rows - 8])
