@@ -20,10 +20,11 @@
 // sum takes it before that.  The output is rounded once.  A masked key has weight zero; where its value is an infinity or NaN the row
 // comes out not finite and is done again by exact_row, which leaves masked values alone.
 //
-// Work item = (request, KV head, part of the key range), with up to 64 stacked rows.  A wavefront has 16 of them: with up to 16 rows the four
-// wavefronts of a workgroup share the item's tiles, with up to 32 two pairs do, with more each takes every tile (the others'
-// loads of it hit in the caches; a wavefront with more rows of its own would have no registers for loads in flight).  They meet in LDS
-// once; parts leave unnormalised sums, references and row sums in slots that few_merge_kernel joins.
+// Work item = (request, KV head, part of the key range), with up to 64 stacked rows.  A wavefront has 16 of them (RB = 1), and with up to 16
+// rows the four wavefronts of a workgroup share the item's tiles, with up to 32 two pairs do, with more each takes every tile, which the
+// others' loads have brought into the caches; or it has 32 (RB = 2), so that tiles are loaded half as often, for 179 registers instead of
+// 120 and longer chains.  They meet in LDS once per 16 rows; parts leave unnormalised sums, references and row sums in slots that
+// few_merge_kernel joins.
 //
 // Measured, us of this kernel (28 query heads, 4 KV heads, d = 128): one token on 2000, 4.1 MB, 6.3 and the merge 3.8, what dependent loads
 // take; 64 single tokens on up to 8000, 468 MB, 83 (5.6 TB/s); 16 on up to 32000, 8 bits, 318 MB, 55 (5.8 TB/s); 24 requests of 3 drafted tokens on
@@ -182,7 +183,7 @@ struct FewUnit {
 };
 
 constexpr int FEW_ONCE = 2;   // cache policy (nt)
-template <int D, bool FP8, bool LIST, class Tab>
+template <int D, bool FP8, bool LIST, int RB, class Tab>
 __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a, Tab tab) {
     typedef FewUnit<D, FP8> U;
     constexpr int KS = D / 32, DT = D / 16, NT = U::SUBS, DTU = DT / U::PER;   // sub-tiles of a K unit, feature blocks of a V unit
@@ -234,8 +235,10 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
     }
     // (a part, and a wavefront's share of it: the quotient, one more for as many of the first as the remainder)
     const int kb0 = n / parts * part + min(part, n % parts), held = n / parts + (part < n % parts);
-    const int rbn = few_row_blocks(rows.rows), rb = wave & (rbn - 1), sharers = FEW_WAVES / rbn, share = wave / rbn;
-    const int slot_blocks = LIST ? rbn : few_row_blocks(min(rq.T * a.g, FEW_GROUP));   // of a part (the last group may have fewer)
+    const int sets = max(few_row_blocks(rows.rows) / RB, 1), set = wave & (sets - 1), sharers = FEW_WAVES / sets, share = wave / sets;
+    const int row0 = set * RB * 16;                                 // a wavefront's first row, of 16 RB
+    const bool two = RB == 2 && rows.rows > row0 + 16;
+    const int slot_blocks = few_row_blocks(LIST ? a.g : min(rq.T * a.g, FEW_GROUP));   // of a part (the last group may have fewer)
     const uint64_t k_head = rq.k + (uint64_t)rows.kvh * (uint32_t)rq.head_tiles * U::TILE;
     const uint64_t v_head = k_head + (uint64_t)a.hkv * (uint32_t)rq.head_tiles * U::TILE;
     const auto tile_at = [&](int i, global_bytes& kt, global_bytes& vt, int& block) RS_INLINE {   // (exact_row's)
@@ -247,29 +250,35 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
     };
 
     // ---- queries
-    bf16x8 qf[KS];
-    int qpos;
-    {
-        const int i = min(rb * 16 + r, rows.rows - 1);   // (rows past the end repeat the last one and are not stored)
-        qpos = rq.P + rows.token(i);
+    bf16x8 qf[RB][KS];
+    int qpos[RB];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+        const int i = min(row0 + b * 16 + r, rows.rows - 1);   // (rows past the end repeat the last one and are not stored)
+        qpos[b] = rq.P + rows.token(i);
         const bf16* p = a.q + (size_t)(rq.row0 + rows.token(i)) * a.ld_q + rows.head(i) * D;
 #pragma unroll
         for (int kk = 0; kk < KS; ++kk)
-            qf[kk] = *reinterpret_cast<const bf16x8*>(p + (FP8 ? (kk >> 1) * 64 + c * 16 + (kk & 1) * 8 : kk * 32 + c * 8));
+            qf[b][kk] = *reinterpret_cast<const bf16x8*>(p + (FP8 ? (kk >> 1) * 64 + c * 16 + (kk & 1) * 8 : kk * 32 + c * 8));
     }
     const int seen_by_all = rq.P + rows.tok0;   // every row of the item sees the keys up to here
     const float sc = FP8 ? a.scale_log2e * rq.k_scale : a.scale_log2e;
 
-    f32x4 acc[DT];
-    float m = -INFINITY, l = 0.0f;
+    f32x4 acc[RB][DT];
+    float m[RB], l[RB];
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) acc[dt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int b = 0; b < RB; ++b) {
+        m[b] = -INFINITY;
+        l[b] = 0.0f;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) acc[b][dt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
     // ---- this wavefront's share of the tiles: neighbours, so that page numbers read across the host link are few lines; of a list every
     // sharers-th, so that wavefronts all over the chip pass the same blocks at about the same time and find them in the L2s.  Their places
     // (page or block) are in a register, a lane each, 64 at a time.
     const int own = held / sharers + (share < held % sharers);
     const int first = kb0 + (LIST ? share : held / sharers * share + min(share, held % sharers)), stride = LIST ? sharers : 1;
-    const int tiles = rb * 16 < rows.rows ? own : 0, last = first + max(own - 1, 0) * stride;
+    const int tiles = row0 < rows.rows ? own : 0, last = first + max(own - 1, 0) * stride;
     int place = 0, number = 0;
     const auto look_up = [&](int j0) RS_INLINE {   // of tiles j0 .. j0 + 63
         const int i = min(first + (j0 + lane) * stride, last);
@@ -328,7 +337,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
     for (int j = 0; j < tiles; ++j) {
         const int key0 = block * 64;
         const bool more = j + 1 < tiles;
-        f32x4 s[4];
+        f32x4 s[RB][4];
         // (the unit after the next: of this tile, or, places looked up in time, of the next one)
         const auto refill = [&](auto hc) RS_INLINE {
             constexpr int h = decltype(hc)::value, n = h + 2;
@@ -362,43 +371,53 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
                     } else {
                         kfrag = as_bf16x8(kf[t * U::K_READS + kk]);
                     }
-                    f32x4& to = s[h * NT + t];
-                    to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kfrag, qf[kk], kk == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : to, 0, 0, 0);
+#pragma unroll
+                    for (int b = 0; b < RB; ++b) {
+                        f32x4& to = s[b][h * NT + t];
+                        to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kfrag, qf[b][kk], kk == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : to, 0, 0, 0);
+                    }
                 }
         });
-        if (key0 + 63 > seen_by_all) {
+        bf16x8 pf[RB][2];
+#pragma unroll
+        for (int b = 0; b < RB; ++b) {
+            if (b > 0 && !two) {   // (no rows: weights of zero)
+                pf[b][0] = pf[b][1] = bf16x8{};
+                continue;
+            }
+            if (key0 + 63 > seen_by_all) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[b][t][e] = key0 + U::key_of(t, c * 4 + e) <= qpos[b] ? s[b][t][e] : -INFINITY;
+            }
+            float mx = s[b][0][0];
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[t][e] = key0 + U::key_of(t, c * 4 + e) <= qpos ? s[t][e] : -INFINITY;
-        }
-        float mx = s[0][0];
+                for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[b][t][e]);
+            mx = of_quarters(mx, larger_of()) * sc;
+            const bool move = mx > m[b] + FEW_HEADROOM;   // (at first m is minus infinity)
+            if (__builtin_amdgcn_ballot_w64(move)) {
+                const float m_new = move ? mx : m[b];
+                const float alpha = m[b] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[b] - m_new);
+                m[b] = m_new;
+                l[b] *= alpha;
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+                for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[t][e]);
-        mx = of_quarters(mx, larger_of()) * sc;
-        const bool move = mx > m + FEW_HEADROOM;   // (at first m is minus infinity)
-        if (__builtin_amdgcn_ballot_w64(move)) {
-            const float m_new = move ? mx : m;
-            const float alpha = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - m_new);
-            m = m_new;
-            l *= alpha;
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[dt][e] *= alpha;
-        }
-        const float ref = m == -INFINITY ? 0.0f : m;
-        bf16x8 pf[2];
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e], sc, -ref));
-                l += p;
-                pf[t >> 1][(t & 1) * 4 + e] = f32_to_bf16(p);
+                    for (int e = 0; e < 4; ++e) acc[b][dt][e] *= alpha;
             }
+            const float ref = m[b] == -INFINITY ? 0.0f : m[b];
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][t][e], sc, -ref));
+                    l[b] += p;
+                    pf[b][t >> 1][(t & 1) * 4 + e] = f32_to_bf16(p);
+                }
+        }
         static_for<0, U::PER>([&](auto hc) RS_INLINE {
             constexpr int h = decltype(hc)::value;
             wait_loads(h + 1 < U::PER || more);
@@ -417,8 +436,11 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
                     bf16x8 vfrag;
                     if constexpr (FP8) vfrag = s2 ? bf16x8_of_codes(vf[dt].z, vf[dt].w) : bf16x8_of_codes(vf[dt].x, vf[dt].y);
                     else vfrag = as_bf16x8(vf[dt * U::V_READS + s2]);
-                    f32x4& to = acc[h * DTU + dt];
-                    to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vfrag, pf[s2], to, 0, 0, 0);
+#pragma unroll
+                    for (int b = 0; b < RB; ++b) {
+                        f32x4& to = acc[b][h * DTU + dt];
+                        to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vfrag, pf[b][s2], to, 0, 0, 0);
+                    }
                 }
         });
         block = __builtin_amdgcn_readlane(number, (j + 1) & 63);
@@ -426,88 +448,97 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
 
     constexpr int SUMS = 16 * (D + 4) * 4;   // bytes of a wavefront's sums
     const auto sums_of = [&](int w, int row) RS_INLINE { return reinterpret_cast<float*>(lds + w * SUMS) + row * (D + 4); };
-    // ---- the wavefronts of the same rows meet: each brings its sums to the largest reference among them
-    l = of_quarters(l, sum_of());
-    if (c == 0) {
-        m_sh[wave][r] = m;
-        l_sh[wave][r] = l;
-    }
-    __syncthreads();
-    float big = m;
-    for (int w = rb; w < FEW_WAVES; w += rbn) big = fmaxf(big, m_sh[w][r]);
-    const float weight = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - big);
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-        f32x4 o = acc[dt];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] *= weight;
-        *reinterpret_cast<f32x4*>(sums_of(wave, r) + dt * 16 + c * 4) = o;
-    }
-    __syncthreads();
     constexpr int PER = D / 16;   // features of a thread
     const int row = threadIdx.x >> 4, f0 = (threadIdx.x & 15) * PER;
-    for (int b = 0; b < rbn && b * 16 < rows.rows; ++b) {
-        float M = -INFINITY, L = 0.0f, o[PER] = {};
-        for (int w = b; w < FEW_WAVES; w += rbn) M = fmaxf(M, m_sh[w][row]);
-        for (int w = b; w < FEW_WAVES; w += rbn) {
-            L += l_sh[w][row] == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(m_sh[w][row] - M) * l_sh[w][row];
-#pragma unroll
-            for (int j = 0; j < PER; ++j) o[j] += sums_of(w, row)[f0 + j];
+    // ---- the wavefronts of the same rows meet: each brings its sums to the largest reference among them
+    static_for<0, RB>([&](auto bc) RS_INLINE {
+        constexpr int own_block = decltype(bc)::value;
+        if (own_block > 0) {
+            if (rows.rows <= 16 * own_block) return;
+            __syncthreads();
         }
-        bool bad = !(fabsf(L) <= 3.402823466e38f);
-#pragma unroll
-        for (int j = 0; j < PER; ++j) {
-            if constexpr (FP8) o[j] *= rq.v_scale;
-            bad |= !(fabsf(o[j]) <= 3.402823466e38f);
+        const float m_own = m[own_block], l_own = of_quarters(l[own_block], sum_of());
+        if (c == 0) {
+            m_sh[wave][r] = m_own;
+            l_sh[wave][r] = l_own;
         }
-        const int i = b * 16 + row;
-        const bool live = i < rows.rows;
-        const int ic = min(i, rows.rows - 1);
-        bf16* const op = a.out + (size_t)(rq.row0 + rows.token(ic)) * a.ld_out + rows.head(ic) * D;
-        float* const slot = a.slots + (size_t)(rq.slot0 + (unit * parts + part) * slot_blocks + b) * FewSlot<D>::FLOATS;
-        const unsigned long long any = __builtin_amdgcn_ballot_w64(bad && live);
-        const bool again = ((any >> (lane & 48)) & 0xffffu) != 0;   // (a row's sixteen threads are neighbours)
-        if (!again && parts > 1) {
+        __syncthreads();
+        float big = m_own;
+        for (int w = set; w < FEW_WAVES; w += sets) big = fmaxf(big, m_sh[w][r]);
+        const float weight = m_own == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_own - big);
 #pragma unroll
-            for (int j = 0; j < PER; j += 4) *reinterpret_cast<f32x4*>(slot + (size_t)row * D + f0 + j) = f32x4{o[j], o[j + 1], o[j + 2], o[j + 3]};
-            if (f0 == 0) {
-                slot[(size_t)16 * D + row] = M;
-                slot[(size_t)16 * (D + 1) + row] = L;
+        for (int dt = 0; dt < DT; ++dt) {
+            f32x4 o = acc[own_block][dt];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] *= weight;
+            *reinterpret_cast<f32x4*>(sums_of(wave, r) + dt * 16 + c * 4) = o;
+        }
+        __syncthreads();
+        for (int sb = 0; sb < sets; ++sb) {
+            const int b = sb * RB + own_block;   // block of 16 rows
+            if (b * 16 >= rows.rows) break;
+            float M = -INFINITY, L = 0.0f, o[PER] = {};
+            for (int w = sb; w < FEW_WAVES; w += sets) M = fmaxf(M, m_sh[w][row]);
+            for (int w = sb; w < FEW_WAVES; w += sets) {
+                L += l_sh[w][row] == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(m_sh[w][row] - M) * l_sh[w][row];
+#pragma unroll
+                for (int j = 0; j < PER; ++j) o[j] += sums_of(w, row)[f0 + j];
             }
-        } else if (!again && live) {
-            const float inv = 1.0f / L;
-            if constexpr (PER == 8) {
-                bf16x8 h;
+            bool bad = !(fabsf(L) <= 3.402823466e38f);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) h[j] = f32_to_bf16(o[j] * inv);
-                *reinterpret_cast<bf16x8*>(op + f0) = h;
-            } else {
-                bf16x4 h;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) h[j] = f32_to_bf16(o[j] * inv);
-                *reinterpret_cast<bf16x4*>(op + f0) = h;
+            for (int j = 0; j < PER; ++j) {
+                if constexpr (FP8) o[j] *= rq.v_scale;
+                bad |= !(fabsf(o[j]) <= 3.402823466e38f);
             }
-        }
-        if (__builtin_expect(any != 0, 0)) {
-            for (int k = 0; k < 4; ++k) {   // the wavefront's four rows
-                if (((any >> (16 * k)) & 0xffffu) == 0) continue;
-                const int bi = b * 16 + wave * 4 + k, tok = rows.token(bi), head = rows.head(bi);
-                float em, el, eo[D / 64];
-                exact_row<D, FP8>(a.q + (size_t)(rq.row0 + tok) * a.ld_q + head * D, sc, rq.P + tok, kb0, kb0 + held, tile_at, em, el, eo);
-                bf16* const bp = a.out + (size_t)(rq.row0 + tok) * a.ld_out + head * D;
+            const int i = b * 16 + row;
+            const bool live = i < rows.rows;
+            const int ic = min(i, rows.rows - 1);
+            bf16* const op = a.out + (size_t)(rq.row0 + rows.token(ic)) * a.ld_out + rows.head(ic) * D;
+            float* const slot = a.slots + (size_t)(rq.slot0 + (unit * parts + part) * slot_blocks + b) * FewSlot<D>::FLOATS;
+            const unsigned long long any = __builtin_amdgcn_ballot_w64(bad && live);
+            const bool again = ((any >> (lane & 48)) & 0xffffu) != 0;   // (a row's sixteen threads are neighbours)
+            if (!again && parts > 1) {
 #pragma unroll
-                for (int j = 0; j < D / 64; ++j) {
-                    const float v = eo[j] * (FP8 ? rq.v_scale : 1.0f);
-                    if (parts > 1) slot[(size_t)(wave * 4 + k) * D + lane + 64 * j] = v;
-                    else bp[lane + 64 * j] = f32_to_bf16(v / el);
+                for (int j = 0; j < PER; j += 4) *reinterpret_cast<f32x4*>(slot + (size_t)row * D + f0 + j) = f32x4{o[j], o[j + 1], o[j + 2], o[j + 3]};
+                if (f0 == 0) {
+                    slot[(size_t)16 * D + row] = M;
+                    slot[(size_t)16 * (D + 1) + row] = L;
                 }
-                if (parts > 1 && lane == 0) {
-                    slot[(size_t)16 * D + wave * 4 + k] = em;
-                    slot[(size_t)16 * (D + 1) + wave * 4 + k] = el;
+            } else if (!again && live) {
+                const float inv = 1.0f / L;
+                if constexpr (PER == 8) {
+                    bf16x8 h;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) h[j] = f32_to_bf16(o[j] * inv);
+                    *reinterpret_cast<bf16x8*>(op + f0) = h;
+                } else {
+                    bf16x4 h;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) h[j] = f32_to_bf16(o[j] * inv);
+                    *reinterpret_cast<bf16x4*>(op + f0) = h;
+                }
+            }
+            if (__builtin_expect(any != 0, 0)) {
+                for (int k = 0; k < 4; ++k) {   // the wavefront's four rows
+                    if (((any >> (16 * k)) & 0xffffu) == 0) continue;
+                    const int bi = b * 16 + wave * 4 + k, tok = rows.token(bi), head = rows.head(bi);
+                    float em, el, eo[D / 64];
+                    exact_row<D, FP8>(a.q + (size_t)(rq.row0 + tok) * a.ld_q + head * D, sc, rq.P + tok, kb0, kb0 + held, tile_at, em, el, eo);
+                    bf16* const bp = a.out + (size_t)(rq.row0 + tok) * a.ld_out + head * D;
+#pragma unroll
+                    for (int j = 0; j < D / 64; ++j) {
+                        const float v = eo[j] * (FP8 ? rq.v_scale : 1.0f);
+                        if (parts > 1) slot[(size_t)(wave * 4 + k) * D + lane + 64 * j] = v;
+                        else bp[lane + 64 * j] = f32_to_bf16(v / el);
+                    }
+                    if (parts > 1 && lane == 0) {
+                        slot[(size_t)16 * D + wave * 4 + k] = em;
+                        slot[(size_t)16 * (D + 1) + wave * 4 + k] = el;
+                    }
                 }
             }
         }
-    }
+    });
 }
 
 // Joins the parts of 16 rows:  M = max_p m_p,  out = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p.  One workgroup per 16 rows and 32

@@ -33,13 +33,17 @@ namespace {
 // KV heads times tiles, all together, up to FEW_TILES; beside requests of few rows, where the chunk kernel's launches come on top of those, up
 // to FEW_TILES_BESIDE; with 8-bit caches, which the chunk kernel needs expanded, up to FEW_TILES_FP8.  us a pass, chunk kernel /
 // attend_few_kernel, (g) 28 query and 4 KV heads, (h) 64 and 8.  One request: (g) 64 tokens on 2000 (896 row groups x heads x tiles)
-// 20.8 / 19.4, 96 on 2000 (1408) 23.0 / 22.0, 96 on 4000 (2772) 26.7 / 28.2, 12 on 20000 (2504) 31.6 / 25.2; (h) 12 on 8000 (2000) 22.9 / 22.2,
-// 32 on 6000 (3008) 26.1 / 28.7, 100 on 2000 (3328) 26.1 / 31.2.  Beside 23 single tokens on 3000: (g) 12 on 5000 (632) 51.4 / 36.9, 24 on 20000
-// (3756) 65.1 / 52.3; (h) 48 on 4000 (3024) 79.1 / 73.4, 24 on 20000 (7512) 93.0 / 94.6; beside 30 on 300: (g) 96 on 4000 (2772) 37.1 / 31.5, (h) 64
-// on 2000 (2048) 37.3 / 30.5, 96 on 4000 (6048) 45.1 / 57.5.  8 bits: (h) 12 on 16000 (4000) 46.5 / 26.8, 100 on 4000 (6552) 40.8 / 43.0; beside
-// 30 on 300, 96 on 4000 (6048) 48.4 / 46.2; beside 60 on 4000, 128 on 4000 (8064) 121.7 / 130.3.
+// 21.1 / 19.4, 96 on 2000 (1408) 23.0 / 22.0, 96 on 4000 (2772) 25.5 / 26.7, 12 on 20000 (2504) 31.6 / 25.2; (h) 12 on 8000 (2000) 22.1 / 21.5,
+// 32 on 6000 (3008) 24.9 / 25.8, 100 on 4000 (6552) 33.0 / 40.4.  Beside 23 single tokens on 3000: (g) 12 on 5000 (632) 51.4 / 36.9, 24 on 20000
+// (3756) 65.1 / 52.3; (h) 48 on 4000 (3024) 79.1 / 73.4; beside 30 on 300: (g) 96 on 4000 (2772) 37.5 / 28.8, (h) 64 on 2000 (2048) 38.4 / 28.0,
+// 96 on 4000 (6048) 46.2 / 54.8; beside 60 on 4000, (g) 128 on 4000 (3528) 109.8 / 100.0, (h) (8064) 184 / 215.  8 bits: (h) 12 on 16000 (4000)
+// 46.9 / 24.6, 100 on 4000 (6552) 41.4 / 37.2; beside 30 on 300, 96 on 4000 (6048) 47.9 / 50.5; beside 60 on 4000, 128 on 4000 (8064) 122.4 / 143.5.
 constexpr int FEW_ROWS = FEW_GROUP;
-constexpr long FEW_TILES = 2000, FEW_TILES_BESIDE = 4500, FEW_TILES_FP8 = 6000;
+constexpr long FEW_TILES = 2500, FEW_TILES_BESIDE = 5000, FEW_TILES_FP8 = 6500;
+// Where a request has more than 32 rows in a group, wavefronts get 32 rows instead of 16 if the call has this many tiles (times KV heads and
+// groups).  us a pass, 16 rows / 32: (h) 16 requests of 5 tokens on up to 8000 (7700) 68.8 / 56.2, 8 bits 47.4 / 39.6; (g) 16 of 8 (3900), 8 bits,
+// 32.4 / 29.8; (h) one of 100 on 4000 (6552) 47.5 / 40.4, 64 on 2000 (2048) 23.0 / 21.6, 8 on 8000 (1000) 20.8 / 21.7, (g) 96 on 2000 (1408) 22.0 / 23.8.
+constexpr long FEW_PAIRS = 2000;
 // Caches that one call reads once are loaded with the streaming hint, unless they are so small that the L2s may still have them from a call
 // before.  us with / without it, behind a fill of 1 GB: 8 MB 14.6 / 15.6, 35 MB 19.6 / 26.6, 141 MB 38.3 / 69.5; call after call on the
 // same caches: 4 MB 15.7 / 14.6, 8 MB 20.2 / 20.4, 141 MB 53.3 / 54.5.
@@ -237,8 +241,8 @@ size_t expansion_bytes(const rs_ctx* c, long tokens) { return (size_t)2 * align_
 // Parts of the key ranges, of `len` tiles at most.  Estimated in tiles of a place (a workgroup's room on a compute unit) when all places stream:
 // an item costs 1.5 beside its tiles, joining 2.  With no more items than places the longest ends last, but the fewer are left the
 // faster they stream: a tile then takes 0.66 of one.  With more, the last ones start late: a share of the longest comes on top.  Where two or
-// all four wavefronts need every tile (16 rows each) it takes 2 and 3 times as long, and parts are that much shorter (us a pass, all
-// alike -> so: 30 single tokens on up to 8000 beside 4 requests of 5 on 3000, 64 query heads, 8 KV heads, 142.7 -> 115.5, 8 bits
+// all four wavefronts need every tile it takes 2 and 3 times as long (wavefronts of 32 rows: 1.5 and 2), and parts are that much shorter (us a
+// pass, all alike -> so: 30 single tokens on up to 8000 beside 4 requests of 5 on 3000, 64 query heads, 8 KV heads, 142.7 -> 115.5, 8 bits
 // 91.3 -> 55.8; 24 requests of 3 on up to 6000 beside one of 12 on 5000 68.4 -> 53.4; one of 4 on 8000, alone, 15.8 -> 17.2).
 // us a pass, parts of 4 / 8 / 16 / 24 / 48 tiles, and with this estimate's: 64 requests on up to 8000 tokens 97.4 / 93.2 / 86.0 / 86.6 / 89.0, 88.3; 16 on up to 32000, 8 bits,
 // 73.2 / 68.6 / 66.1 / 64.6 / 59.4, 60.2; 24 of 3 tokens on up to 6000 and one of 12, 64 and 8 heads, 79.6 / 69.5 / 58.3 / 56.6 / 67.0, 54.3.
@@ -248,16 +252,16 @@ struct FewRequest {
     int row_blocks;        // of 16 rows: 1, 2 or 4
     int parts;
     bool once = false;     // its tiles are read once
-    int weight() const { return row_blocks == 1 ? 1 : row_blocks == 2 ? 2 : 3; }   // of a tile
-    long work() const { return (long)tiles * weight(); }
-    int parts_of(int len) const { return (int)std::min<long>((work() + len - 1) / len, FEW_MAX_PARTS); }
+    double weight = 1.0;   // of a tile
+    double work() const { return tiles * weight; }
+    int parts_of(int len) const { return std::min((int)std::ceil(work() / len), FEW_MAX_PARTS); }
 };
 void plan_few(std::vector<FewRequest>& reqs, int places, size_t slots) {
-    long total = 0;
+    double total = 0.0;
     int longest = 1;
     for (const FewRequest& r : reqs) {
         total += r.units * r.work();
-        longest = std::max(longest, (int)r.work());
+        longest = std::max(longest, (int)std::ceil(r.work()));
     }
     double best = 1e30;
     int best_len = longest;
@@ -268,9 +272,9 @@ void plan_few(std::vector<FewRequest>& reqs, int places, size_t slots) {
             const int p = r.parts_of(len);
             items += (long)r.units * p;
             if (p > 1) split += (long)r.units * p * r.row_blocks;
-            most = std::max(most, (r.tiles + p - 1) / p * r.weight() * 0.66);
+            most = std::max(most, (r.tiles + p - 1) / p * r.weight * 0.66);
         }
-        const double share = (double)total / places;
+        const double share = total / places;
         const double cost = (items <= places ? std::max(share, most) + 1.5 : share + 1.5 * items / places + 0.5 * most) + (split ? 2.0 : 0.0);
         if ((size_t)split <= slots && cost < best) {
             best = cost;
@@ -326,10 +330,14 @@ size_t few_table_pages(rs_kv* const* kvs, const std::vector<FewRequest>& reqs) {
 }
 
 template <bool LIST, class Tab>
-rs_status launch_few(const rs_ctx* ctx, bool fp8, const FewArgs& a, uint32_t items, uint32_t units, bool split, const Tab& tab, hipStream_t st) {
+rs_status launch_few(const rs_ctx* ctx, bool fp8, bool pairs, const FewArgs& a, uint32_t items, uint32_t units, bool split, const Tab& tab, hipStream_t st) {
     for_kind(ctx, fp8, [&](auto d, auto f8) {
         constexpr int D = decltype(d)::value;
-        hipLaunchKernelGGL((attend_few_kernel<D, decltype(f8)::value, LIST, Tab>), dim3(items), dim3(64 * FEW_WAVES), 0, st, a, tab);
+        constexpr bool FP8 = decltype(f8)::value;
+        const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(items), dim3(64 * FEW_WAVES), 0, st, a, tab); };
+        if constexpr (LIST) launch(attend_few_kernel<D, FP8, true, 1, Tab>);
+        else if (pairs) launch(attend_few_kernel<D, FP8, false, 2, Tab>);
+        else launch(attend_few_kernel<D, FP8, false, 1, Tab>);
         if (split) hipLaunchKernelGGL((few_merge_kernel<D, LIST, Tab>), dim3(units, D / 32), dim3(256), 0, st, a, tab);
     });
     RS_HIP(hipGetLastError());
@@ -649,11 +657,21 @@ rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, 
     FewArgs a{};
     FewTable ft;
     InlineTable tab;
+    bool pairs = false;                  // wavefronts have two blocks of 16 rows
     enum { NOTHING, PAGES, ALL } few_staged = NOTHING;   // of the table (see TABLE_WORDS)
     size_t few_words = 0, few_pages = 0, few_bytes = 0;   // few_bytes: of the keys and values they read
     if (!few.empty()) {
         for (const FewRequest& r : few) few_bytes += (size_t)r.tiles * 128 * ctx->kv_dim * (fp8 ? 1 : 2);
-        for (FewRequest& r : few) r.once = few_bytes >= FEW_ONCE_BYTES && r.row_blocks == 1;
+        long all_tiles = 0;
+        for (const FewRequest& r : few) {
+            pairs |= r.row_blocks > 2;
+            all_tiles += (long)r.units * r.tiles;
+        }
+        pairs = pairs && all_tiles >= FEW_PAIRS;
+        for (FewRequest& r : few) {
+            r.once = few_bytes >= FEW_ONCE_BYTES && r.row_blocks == 1;
+            r.weight = pairs ? (r.row_blocks == 1 ? 1.0 : r.row_blocks == 2 ? 1.5 : 2.0) : (r.row_blocks == 1 ? 1.0 : r.row_blocks == 2 ? 2.0 : 3.0);
+        }
         plan_few(few, FEW_PLACES * ctx->n_cu, SLOT_ROWS / 16);
         a.n_req = (int)few.size();
         a.hkv = f.n_kv_heads; a.g = ctx->group;
@@ -742,7 +760,7 @@ rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, 
         if (a.pages) a.pages = reinterpret_cast<const uint32_t*>(ws);   // (copied too)
     }
     if (!few.empty()) {
-        const auto launch = [&](const auto& table) { s = launch_few<false>(ctx, fp8, a, ft.items, ft.units, ft.any_split, table, st); };
+        const auto launch = [&](const auto& table) { s = launch_few<false>(ctx, fp8, pairs, a, ft.items, ft.units, ft.any_split, table, st); };
         if (few_staged == ALL) launch(NoTable{});
         else with_table(tab, few_words + (few_staged == NOTHING ? few_pages : 0), launch);
         if (s != RS_OK) return s;
@@ -953,7 +971,7 @@ rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int*
     a.chosen = list;
     a.n_blocks = n_blocks;
     a.list_parts = parts;
-    return launch_few<true>(ctx, fp8, a, (uint32_t)(units * parts), (uint32_t)(units * rbn), parts > 1, NoTable{}, st);
+    return launch_few<true>(ctx, fp8, false, a, (uint32_t)(units * parts), (uint32_t)(units * rbn), parts > 1, NoTable{}, st);
 } catch (const std::exception& e) {
     return not_allocated(e);
 }
