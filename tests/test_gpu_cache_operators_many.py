@@ -134,3 +134,38 @@ def test_masked_values_that_are_not_finite_in_lists_in_parts():
     out, chosen = T.run_blocks(ctx, [kv], [rows], q, 40, 1, 2)
     ref, mag = O.attend(T.f64(q).reshape(rows, hq, d), T.f64(k), T.f64(v), n - rows)
     T.assert_attention(out[:rows - 8], ref[:rows - 8], mag[:rows - 8])
+
+
+@pytest.mark.parametrize("kind", T.KINDS)
+@pytest.mark.parametrize("hq, hkv, d", [(64, 8, 64), (28, 4, 128), (40, 2, 128)])
+def test_drafts_on_much_cache(kind, hq, hkv, d):
+    """Requests of 33 to 64 rows and more in calls with so much to read that wavefronts have 32 rows, beside single tokens and few drafts."""
+    ctx = T.context(hq, hkv, d)
+    per_head = 2100 // hkv * 64 // 6
+    lens = [5, 1, 12, 8, 3, 0, 7, 2, 1, 16]
+    held = [per_head + 171 * i for i in range(6)] + [300, 40, 1, 16]
+    kvs, content, g = filled(ctx, kind, held, 66, d, hkv)
+    check_attend(ctx, kind, kvs, content, held, lens, g)
+
+
+@pytest.mark.parametrize("kind", ["contiguous", "paged"])
+def test_what_drafts_on_much_cache_do_not_see_does_not_reach_them(kind):
+    """Infinities and NaN behind the rows' own slots, in their blocks; wavefronts of 32 rows."""
+    hq, hkv, d = 64, 8, 64
+    ctx = T.context(hq, hkv, d)
+    g = T.gen(67)
+    n, rows = 17011, 8
+    kv, = T.caches(ctx, kind, [n])
+    k, v = T.normal(g, n, hkv, d), T.normal(g, n, hkv, d)
+    dirty_k, dirty_v = k.clone(), v.clone()
+    dirty_v[-3:, 0] = float("nan")
+    dirty_v[-2:, 1, 7] = float("inf")
+    dirty_k[-1:, 2] = float("-inf")
+    kv.import_(0, dirty_k, dirty_v)
+    q = T.normal(g, rows, hq * d, std=1.5)
+    out = torch.full_like(q, float("nan"))
+    ctx.attend(0, [kv], [rows], q, out, ctx.attend_workspace(rows))
+    ref, mag = O.attend(T.f64(q).reshape(rows, hq, d), T.f64(k), T.f64(v), n - rows)
+    T.assert_attention(out[: rows - 3], ref[: rows - 3], mag[: rows - 3])
+    group = hq // hkv * d   # (the other KV heads' rows are whole to the last)
+    T.assert_attention(out[:, 3 * group:].reshape(rows, hq - 3 * (hq // hkv), d), ref[:, 3 * (hq // hkv):], mag[:, 3 * (hq // hkv):])
