@@ -28,7 +28,7 @@
 //
 // Measured, us of this kernel (28 query heads, 4 KV heads, d = 128): one token on 2000, 4.1 MB, 6.3 and the merge 3.8, what dependent loads
 // take; 64 single tokens on up to 8000, 468 MB, 83 (5.6 TB/s); 16 on up to 32000, 8 bits, 318 MB, 55 (5.8 TB/s); 24 requests of 3 drafted tokens on
-// up to 6000 and one of 12, 64 and 8 heads, 240 MB, 47 (5.1 TB/s); 256 tokens with 32 selected blocks each, 1.07 GB from the L2s (90 %
+// up to 6000 and one of 12, 64 and 8 heads, 240 MB, 46 to 47 (5.1 TB/s, RB = 2); 256 tokens with 32 selected blocks each, 1.07 GB from the L2s (90 %
 // of the reads hit), 46 to 48 (23 TB/s: LDS, which takes and gives every byte, is busy for 60 % of that).
 #pragma once
 #include "attention.h"

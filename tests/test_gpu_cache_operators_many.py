@@ -169,3 +169,26 @@ def test_what_drafts_on_much_cache_do_not_see_does_not_reach_them(kind):
     T.assert_attention(out[: rows - 3], ref[: rows - 3], mag[: rows - 3])
     group = hq // hkv * d   # (the other KV heads' rows are whole to the last)
     T.assert_attention(out[:, 3 * group:].reshape(rows, hq - 3 * (hq // hkv), d), ref[:, 3 * (hq // hkv):], mag[:, 3 * (hq // hkv):])
+
+
+@pytest.mark.parametrize("rule", ["0", "1000000"])
+def test_out_may_be_q(rule, monkeypatch):
+    """The same bits whether the output goes to memory of its own or over the queries."""
+    monkeypatch.setenv("RS_ATTEND_FEW", rule)
+    hq, hkv, d = 28, 4, 128
+    ctx = T.context(hq, hkv, d)
+    held, lens = [3000, 700, 90, 400], [1, 5, 40, 150]
+    kvs, content, g = filled(ctx, "paged", held, 68, d, hkv)
+    q = T.normal(g, sum(lens), hq * d)
+    ws = ctx.attend_workspace(sum(lens), len(held))
+    out, over = torch.empty_like(q), q.clone()
+    ctx.attend(0, kvs, lens, q, out, ws)
+    ctx.attend(0, kvs, lens, over, over, ws)
+    assert torch.equal(out, over)
+    for kv, n in zip(kvs, held):
+        kv.new_bounds(n + 64)
+    ws = ctx.attend_workspace(sum(lens), len(held), n_blocks=20)
+    over = q.clone()
+    ctx.attend_blocks(0, kvs, lens, q, out, ws, 20)
+    ctx.attend_blocks(0, kvs, lens, over, over, ws, 20)
+    assert torch.equal(out, over)
