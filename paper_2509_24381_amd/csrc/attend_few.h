@@ -122,7 +122,7 @@ constexpr int FEW_GROUP = 64;          // stacked rows of an item
 // An item's rows, and where they are in q and out.
 template <bool LIST>
 struct FewRows {
-    int row0, P, kvh, g, first, tok0, rows;   // first: of the request's stacked rows; tok0: its token.  (LIST: the g heads of one token)
+    int kvh, g, first, tok0, rows;   // first: of the request's stacked rows; tok0: its token.  (LIST: the g heads of one token)
     __device__ __forceinline__ int token(int i) const { return LIST ? tok0 : (first + i) / g; }
     __device__ __forceinline__ int head(int i) const { return kvh * g + (LIST ? i : (first + i) % g); }
     // Takes the rows of group `group` of a request's `all`.
@@ -183,56 +183,19 @@ struct FewUnit {
 };
 
 constexpr int FEW_ONCE = 2;   // cache policy (nt)
-template <int D, bool FP8, bool LIST, int RB, class Tab>
-__global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a, Tab tab) {
+// LDS of a workgroup: each wavefront's keys and values, in the end all their sums; and, apart from it (the compiler waits for the DMA into
+// whatever it cannot tell from what it reads), references and row sums.
+template <int D, bool FP8>
+constexpr int FEW_LDS = FEW_WAVES * (2 * FewUnit<D, FP8>::BYTES > 16 * (D + 4) * 4 ? 2 * FewUnit<D, FP8>::BYTES : 16 * (D + 4) * 4);
+typedef float FewStats[FEW_WAVES][16];
+// Part `part` of `parts` of an item of n tiles, or of a list's n blocks: unit `unit` of its request (of all, with lists) writes its rows or slots.
+template <int D, bool FP8, bool LIST, int RB>
+RS_DEVICE void attend_rows(const FewArgs& a, const FewReq& rq, const uint32_t* pages, const FewRows<LIST>& rows, int part, int parts, int unit, int n,
+                           const int* list, char* lds, FewStats& m_sh, FewStats& l_sh) {
     typedef FewUnit<D, FP8> U;
     constexpr int KS = D / 32, DT = D / 16, NT = U::SUBS, DTU = DT / U::PER;   // sub-tiles of a K unit, feature blocks of a V unit
-    // each wavefront's keys and values, in the end all their sums
-    constexpr int LDS_BYTES = FEW_WAVES * (2 * U::BYTES > 16 * (D + 4) * 4 ? 2 * U::BYTES : 16 * (D + 4) * 4);
-    __shared__ __attribute__((aligned(16))) char lds[LDS_BYTES];
-    __shared__ float m_sh[FEW_WAVES][16], l_sh[FEW_WAVES][16];
-    const uint32_t* const table = table_of(tab, a.table);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, c = lane >> 4;
-
-    // ---- which rows, which tiles
-    FewRows<LIST> rows;
-    int req, part, parts, unit, n;   // n: tiles, or blocks of the list
-    const int* list = nullptr;
-    rows.g = a.g;
-    if constexpr (LIST) {
-        int id = blockIdx.x;
-        rows.kvh = id % a.hkv;
-        id /= a.hkv;
-        parts = a.list_parts;
-        part = id % parts;
-        const int row = id / parts;
-        req = request_of(table, a.n_req, (uint32_t)row);
-        unit = row * a.hkv + rows.kvh;
-        rows.tok0 = row;
-        rows.rows = a.g;
-    } else {
-        req = request_of(table, a.n_req, blockIdx.x);
-        unit = part = parts = 0;
-    }
-    const FewReq rq = reinterpret_cast<const FewReq*>(table + table_reqs_at(a.n_req))[req];
-    const uint32_t* const pages = a.pages ? a.pages : table + table_reqs_at(a.n_req) + REQ_WORDS * a.n_req;
-    rows.row0 = rq.row0;
-    rows.P = rq.P;
-    if constexpr (LIST) {
-        rows.tok0 -= rq.row0;
-        list = a.chosen + (size_t)unit * a.n_blocks;
-        n = min(a.n_blocks, (rq.P + rows.tok0) / 64 + 1);   // (the list ends there)
-    } else {
-        int id = (int)(blockIdx.x - table[req]);
-        parts = rq.parts;
-        rows.kvh = id % a.hkv;
-        id /= a.hkv;
-        part = id % parts;
-        rows.take(id / parts, rq.T * a.g);
-        unit = id / parts * a.hkv + rows.kvh;
-        n = (rq.P + rows.token(rows.rows - 1)) / 64 + 1;
-    }
     // (a part, and a wavefront's share of it: the quotient, one more for as many of the first as the remainder)
     const int kb0 = n / parts * part + min(part, n % parts), held = n / parts + (part < n % parts);
     const int sets = max(few_row_blocks(rows.rows) / RB, 1), set = wave & (sets - 1), sharers = FEW_WAVES / sets, share = wave / sets;
@@ -539,6 +502,46 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
             }
         }
     });
+}
+
+template <int D, bool FP8, bool LIST, int RB, class Tab>
+__global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a, Tab tab) {
+    __shared__ __attribute__((aligned(16))) char lds[FEW_LDS<D, FP8>];
+    __shared__ FewStats m_sh, l_sh;
+    const uint32_t* const table = table_of(tab, a.table);
+    FewRows<LIST> rows;
+    int id = blockIdx.x, req, part, parts, unit, n;   // n: tiles, or blocks of the list
+    const int* list = nullptr;
+    rows.g = a.g;
+    if constexpr (LIST) {
+        rows.kvh = id % a.hkv;
+        id /= a.hkv;
+        parts = a.list_parts;
+        part = id % parts;
+        rows.tok0 = id / parts;
+        req = request_of(table, a.n_req, (uint32_t)rows.tok0);
+        unit = rows.tok0 * a.hkv + rows.kvh;
+    } else {
+        req = request_of(table, a.n_req, blockIdx.x);
+    }
+    const FewReq rq = reinterpret_cast<const FewReq*>(table + table_reqs_at(a.n_req))[req];
+    const uint32_t* const pages = a.pages ? a.pages : table + table_reqs_at(a.n_req) + REQ_WORDS * a.n_req;
+    if constexpr (LIST) {
+        rows.tok0 -= rq.row0;
+        rows.rows = a.g;
+        list = a.chosen + (size_t)unit * a.n_blocks;
+        n = min(a.n_blocks, (rq.P + rows.tok0) / 64 + 1);   // (the list ends there)
+    } else {
+        id -= (int)table[req];
+        parts = rq.parts;
+        rows.kvh = id % a.hkv;
+        id /= a.hkv;
+        part = id % parts;
+        rows.take(id / parts, rq.T * a.g);
+        unit = id / parts * a.hkv + rows.kvh;
+        n = (rq.P + rows.token(rows.rows - 1)) / 64 + 1;
+    }
+    attend_rows<D, FP8, LIST, RB>(a, rq, pages, rows, part, parts, unit, n, list, lds, m_sh, l_sh);
 }
 
 // Joins the parts of 16 rows:  M = max_p m_p,  out = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p.  One workgroup per 16 rows and 32

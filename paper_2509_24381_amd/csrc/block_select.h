@@ -219,17 +219,167 @@ RS_DEVICE uint32_t cut_of_keys(const uint32_t* key, int lo, int hi, int take, Se
 
 constexpr int SELECT_U = 4;                            // groups of 16 blocks that a wavefront has in flight
 constexpr int SELECT_ROUND = 4 * 16 * SELECT_U;        // blocks that a workgroup scores at a time
+// Scores of blocks [s0, s1) for nt <= TOKENS tokens, whose queries of the KV head start at q, as keys into `to`: by four wavefronts, from s0 +
+// start on, `step` further each time.  u: the tokens' p and n.
+template <int D, int TOKENS>
+RS_DEVICE void score_blocks(const bf16* q, long ld_q, int g, int halvings, int nt, const int8_t* codes, const float* units, int s0, int s1, int start, int step,
+                            int8_t (*u)[2 * D], uint32_t* to, int ld_to) {
+    constexpr int KK = 2 * D / 64, U = SELECT_U;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int W = D / 64;   // features of a lane: W lane ..
+    const int r = lane & 15, c = lane >> 4;
+    i32x4 x[U][KK];
+    float unit[U];
+    const auto load = [&](int b) RS_INLINE {   // bounds of the wavefront's blocks b ..
+#pragma unroll
+        for (int v = 0; v < U; ++v) {
+            const int block = min(b + v * 16 + r, s1 - 1);
+            const int8_t* const src = codes + (size_t)block * 2 * D + c * 16;
+#pragma unroll
+            for (int k = 0; k < KK; ++k) x[v][k] = *reinterpret_cast<const i32x4*>(src + k * 64);
+            unit[v] = units[block];
+        }
+    };
+    // a wavefront's token, eight heads at a time, their loads in flight together and before the bounds'
+    const bf16* const query = q + (size_t)min(wave, nt - 1) * ld_q + lane * W;
+    typedef __attribute__((ext_vector_type(W))) __bf16 heads_t;
+    heads_t qh[8];
+    const auto load_heads = [&](int i0) RS_INLINE {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) qh[i] = *reinterpret_cast<const heads_t*>(query + (size_t)min(i0 + i, g - 1) * D);
+    };
+    load_heads(0);
+    int b = s0 + start + wave * 16 * U;
+    load(b);   // (under way while the queries become codes)
+    if (wave < nt) {
+        int p[W] = {}, n[W] = {};
+        float top = 0.0f;
+        for (int i0 = 0;;) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int j = 0; j < W; ++j) top = fmaxf(top, fabsf(limited((float)qh[i][j])));
+            i0 += 8;
+            if (i0 >= g) break;
+            load_heads(i0);
+        }
+        const int ex = code_exponent(of_wave(top, larger_of()));
+        for (int i0 = 0; i0 < g; i0 += 8) {
+            if (g > 8) load_heads(i0);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int j = 0; j < W; ++j) {
+                    const int code = i0 + i < g ? (int)rintf(__builtin_ldexpf(limited((float)qh[i][j]), -ex)) : 0;
+                    p[j] += max(code, 0);
+                    n[j] += max(-code, 0);
+                }
+        }
+        const int half = (1 << halvings) >> 1;
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            u[wave][lane * W + j] = (int8_t)((p[j] + half) >> halvings);
+            u[wave][D + lane * W + j] = (int8_t)(-((n[j] + half) >> halvings));
+        }
+    }
+    __syncthreads();
+    i32x4 uf[KK];   // (rows past the tokens' are not used)
+#pragma unroll
+    for (int k = 0; k < KK; ++k) uf[k] = *reinterpret_cast<const i32x4*>(&u[TOKENS == 1 ? 0 : r & 3][k * 64 + c * 16]);
+    while (b < s1) {
+#pragma unroll
+        for (int v = 0; v < U; ++v) {
+            i32x4 dot = {0, 0, 0, 0};
+#pragma unroll
+            for (int k = 0; k < KK; ++k) dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(uf[k], x[v][k], dot, 0, 0, 0);
+            const int block = b + v * 16 + r;   // token 4 c + e
+            if (c == 0 && block < s1)
+#pragma unroll
+                for (int e = 0; e < TOKENS; ++e)
+                    if (e < nt) to[e * ld_to + block - s0] = key_of_score((float)dot[e] * unit[v]);
+        }
+        b += step;
+        if (b < s1) load(b);
+    }
+}
+
+// The blocks that a token whose own block is `own` attends to, ascending, -1 behind the last of n_blocks; key[b]: block b's score.  A team of TEAM
+// wavefronts; chunk_more, chunk_equal: a word per 64 blocks each (TEAM > 1).
+template <int TEAM>
+RS_DEVICE void pick_blocks(const uint32_t* key, int own, int n_blocks, int n_first, int n_last, SelectTeam<TEAM>& sh, uint32_t* chunk_more, uint32_t* chunk_equal,
+                           int* out) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned long long below = lane == 0 ? 0ull : ~0ull >> (64 - lane);   // the lanes before this one
+    const int lo = min(n_first, own + 1), hi = max(lo, own + 1 - n_last);   // blocks lo .. hi - 1 compete
+    const int take = min(max(n_blocks - (own + 1 - (hi - lo)), 0), hi - lo);
+    uint32_t cut = 0;   // the take-th largest key; of the blocks that have it, the first `equals`
+    int equals = 0;
+    const bool some = take > 0 && take < hi - lo;
+    if (some) cut = cut_of_keys<TEAM>(key, lo, hi, take, sh, &equals);
+    // is block b taken for sure; does it have the cut's key
+    const auto taken = [&](int b, bool& eq) RS_INLINE {
+        const bool competes = b >= lo && b < hi;
+        const uint32_t k = some && competes ? key[b] : 0u;
+        eq = some && competes && k == cut;
+        return competes ? (some ? k > cut : take > 0) : b <= own;
+    };
+    const int chunks = own / 64 + 1;   // of 64 blocks
+    if constexpr (TEAM == 1) {
+        int done = 0;
+        for (int ch = 0; ch < chunks && done < n_blocks; ++ch) {
+            bool eq;
+            bool sel = taken(ch * 64 + lane, eq);
+            const unsigned long long eqs = __builtin_amdgcn_ballot_w64(eq);
+            if (eq) sel = __popcll(eqs & below) < equals;
+            equals -= min(equals, (int)__popcll(eqs));
+            const unsigned long long sels = __builtin_amdgcn_ballot_w64(sel);
+            const int at = done + (int)__popcll(sels & below);
+            if (sel && at < n_blocks) out[at] = ch * 64 + lane;
+            done += (int)__popcll(sels);
+        }
+        for (int i = min(done, n_blocks) + lane; i < n_blocks; i += 64) out[i] = -1;
+    } else {
+        for (int ch = wave; ch < chunks; ch += TEAM) {
+            bool eq;
+            const bool sel = taken(ch * 64 + lane, eq);
+            const uint32_t more = (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(sel)), equal = (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(eq));
+            if (lane == 0) {
+                chunk_more[ch] = more;
+                chunk_equal[ch] = equal;
+            }
+        }
+        __syncthreads();
+        for (int ch = wave; ch < chunks; ch += TEAM) {
+            int more = 0, equal = 0;   // in the chunks before this one
+            for (int i = lane; i < ch; i += 64) {
+                more += (int)chunk_more[i];
+                equal += (int)chunk_equal[i];
+            }
+            more = of_wave(more, sum_of());
+            equal = of_wave(equal, sum_of());
+            bool eq;
+            bool sel = taken(ch * 64 + lane, eq);
+            if (eq) sel = equal + (int)__popcll(__builtin_amdgcn_ballot_w64(eq) & below) < equals;
+            const unsigned long long sels = __builtin_amdgcn_ballot_w64(sel);
+            const int at = more + min(equal, equals) + (int)__popcll(sels & below);
+            if (sel && at < n_blocks) out[at] = ch * 64 + lane;
+        }
+        const int all = min(n_blocks, own + 1);
+        for (int i = all + (int)threadIdx.x; i < n_blocks; i += 64 * TEAM) out[i] = -1;
+    }
+}
+
 enum SelectSteps { SELECT_ALL = 0, SELECT_SCORES = 1, SELECT_FROM_SCORES = 2 };
 template <int D, bool WIDE, int STEPS, class Tab>
 __global__ __launch_bounds__(STEPS == SELECT_FROM_SCORES ? 1024 : 256) void block_select_kernel(SelectArgs a, Tab tab) {
     static_assert(WIDE || STEPS == SELECT_ALL, "only few tokens take two launches");
-    constexpr int WAVES = STEPS == SELECT_FROM_SCORES ? 16 : 4, TEAM = WIDE ? WAVES : 1, TEAMS = WAVES / TEAM, KK = 2 * D / 64, U = SELECT_U;
+    constexpr int WAVES = STEPS == SELECT_FROM_SCORES ? 16 : 4, TEAM = WIDE ? WAVES : 1, TEAMS = WAVES / TEAM;
     extern __shared__ __attribute__((aligned(16))) uint32_t keys[];   // [tokens][blocks]
     __shared__ __attribute__((aligned(16))) int8_t u[4][2 * D];
     __shared__ __attribute__((aligned(16))) SelectTeam<TEAM> team_sh[TEAMS];
     __shared__ uint32_t chunk_more[TEAM == 1 ? 1 : SELECT_MAX_BLOCKS / 64], chunk_equal[TEAM == 1 ? 1 : SELECT_MAX_BLOCKS / 64];
     const uint32_t* const table = tab.w;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = blockIdx.y;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = blockIdx.y;
     if (STEPS != SELECT_FROM_SCORES && (int)blockIdx.x >= a.groups) {
         const int i = ((int)blockIdx.x - a.groups) * 64 * WAVES + (int)threadIdx.x;
         if (h == 0 && i < a.copy_chunks) a.copy_to[i] = a.copy_from[i];
@@ -245,152 +395,18 @@ __global__ __launch_bounds__(STEPS == SELECT_FROM_SCORES ? 1024 : 256) void bloc
     const bool scored = b_last + 1 > a.n_blocks && s1 > s0;   // (else every token takes all it has, or none but the forced ones)
     uint32_t* const shared = STEPS == SELECT_ALL ? nullptr : a.shared_keys + ((size_t)(rq.row0 + t0) * a.hkv + h) * a.blocks;
     uint32_t* const to = STEPS == SELECT_SCORES ? shared : keys;   // where the scores' keys go
-    if (STEPS == SELECT_FROM_SCORES && scored) {
-        for (int i = threadIdx.x * 4; i < s1 - s0; i += 64 * WAVES * 4) *reinterpret_cast<uint4*>(&keys[i]) = *reinterpret_cast<const uint4*>(&shared[i]);
-        __syncthreads();
-    }
-    if (STEPS != SELECT_FROM_SCORES && scored) {
-        constexpr int W = D / 64;   // features of a lane: W lane ..
-        const int r = lane & 15, c = lane >> 4;
-        const int8_t* const codes = reinterpret_cast<const int8_t*>(rq.codes) + (size_t)h * rq.room * 2 * D;
-        const float* const units = reinterpret_cast<const float*>(rq.units) + (size_t)h * rq.room;
-        i32x4 x[U][KK];
-        float unit[U];
-        const auto load = [&](int b) RS_INLINE {   // bounds of the wavefront's blocks b ..
-#pragma unroll
-            for (int v = 0; v < U; ++v) {
-                const int block = min(b + v * 16 + r, s1 - 1);
-                const int8_t* const src = codes + (size_t)block * 2 * D + c * 16;
-#pragma unroll
-                for (int k = 0; k < KK; ++k) x[v][k] = *reinterpret_cast<const i32x4*>(src + k * 64);
-                unit[v] = units[block];
-            }
-        };
-        // a wavefront's token, eight heads at a time, their loads in flight together and before the bounds'
-        const bf16* const query = a.q + (size_t)(rq.row0 + t0 + min(wave, nt - 1)) * a.ld_q + (size_t)h * a.g * D + lane * W;
-        typedef __attribute__((ext_vector_type(W))) __bf16 heads_t;
-        heads_t qh[8];
-        const auto load_heads = [&](int i0) RS_INLINE {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) qh[i] = *reinterpret_cast<const heads_t*>(query + (size_t)min(i0 + i, a.g - 1) * D);
-        };
-        load_heads(0);
-        int b = s0 + share * SELECT_ROUND + wave * 16 * U;
-        load(b);   // (under way while the queries become codes)
-        if (wave < nt) {
-            int p[W] = {}, n[W] = {};
-            float top = 0.0f;
-            for (int i0 = 0;;) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-#pragma unroll
-                    for (int j = 0; j < W; ++j) top = fmaxf(top, fabsf(limited((float)qh[i][j])));
-                i0 += 8;
-                if (i0 >= a.g) break;
-                load_heads(i0);
-            }
-            const int ex = code_exponent(of_wave(top, larger_of()));
-            for (int i0 = 0; i0 < a.g; i0 += 8) {
-                if (a.g > 8) load_heads(i0);
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-#pragma unroll
-                    for (int j = 0; j < W; ++j) {
-                        const int code = i0 + i < a.g ? (int)rintf(__builtin_ldexpf(limited((float)qh[i][j]), -ex)) : 0;
-                        p[j] += max(code, 0);
-                        n[j] += max(-code, 0);
-                    }
-            }
-            const int half = (1 << a.halvings) >> 1;
-#pragma unroll
-            for (int j = 0; j < W; ++j) {
-                u[wave][lane * W + j] = (int8_t)((p[j] + half) >> a.halvings);
-                u[wave][D + lane * W + j] = (int8_t)(-((n[j] + half) >> a.halvings));
-            }
-        }
-        __syncthreads();
-        i32x4 uf[KK];   // (rows past the tokens' are not used)
-#pragma unroll
-        for (int k = 0; k < KK; ++k) uf[k] = *reinterpret_cast<const i32x4*>(&u[WIDE ? 0 : r & 3][k * 64 + c * 16]);
-        while (b < s1) {
-#pragma unroll
-            for (int v = 0; v < U; ++v) {
-                i32x4 dot = {0, 0, 0, 0};
-#pragma unroll
-                for (int k = 0; k < KK; ++k) dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(uf[k], x[v][k], dot, 0, 0, 0);
-                const int block = b + v * 16 + r;   // token 4 c + e
-                if (c == 0 && block < s1)
-#pragma unroll
-                    for (int e = 0; e < (WIDE ? 1 : 4); ++e)
-                        if (e < nt) to[e * a.blocks + block - s0] = key_of_score((float)dot[e] * unit[v]);
-            }
-            b += split * SELECT_ROUND;
-            if (b < s1) load(b);
-        }
+    if (scored) {
+        if constexpr (STEPS == SELECT_FROM_SCORES)
+            for (int i = threadIdx.x * 4; i < s1 - s0; i += 64 * WAVES * 4) *reinterpret_cast<uint4*>(&keys[i]) = *reinterpret_cast<const uint4*>(&shared[i]);
+        else
+            score_blocks<D, WIDE ? 1 : 4>(a.q + (size_t)(rq.row0 + t0) * a.ld_q + (size_t)h * a.g * D, a.ld_q, a.g, a.halvings, nt,
+                                          reinterpret_cast<const int8_t*>(rq.codes) + (size_t)h * rq.room * 2 * D,
+                                          reinterpret_cast<const float*>(rq.units) + (size_t)h * rq.room, s0, s1, share * SELECT_ROUND, split * SELECT_ROUND, u, to,
+                                          a.blocks);
         __syncthreads();
     }
     if constexpr (STEPS == SELECT_SCORES) return;
-    const unsigned long long below = lane == 0 ? 0ull : ~0ull >> (64 - lane);   // the lanes before this one
-    for (int t = TEAM == 1 ? wave : 0; t < nt; t += TEAMS) {
-        const int own = (rq.P + t0 + t) / 64;
-        const int lo = min(a.n_first, own + 1), hi = max(lo, own + 1 - a.n_last);   // blocks lo .. hi - 1 compete
-        const int take = min(max(a.n_blocks - (own + 1 - (hi - lo)), 0), hi - lo);
-        const uint32_t* const key = keys + t * a.blocks - s0;
-        uint32_t cut = 0;   // the take-th largest key; of the blocks that have it, the first `equals`
-        int equals = 0;
-        const bool some = take > 0 && take < hi - lo;
-        if (some) cut = cut_of_keys<TEAM>(key, lo, hi, take, team_sh[TEAM == 1 ? wave : 0], &equals);
-        int* const out = a.chosen + ((size_t)(rq.row0 + t0 + t) * a.hkv + h) * a.n_blocks;
-        // is block b taken for sure; does it have the cut's key
-        const auto taken = [&](int b, bool& eq) RS_INLINE {
-            const bool competes = b >= lo && b < hi;
-            const uint32_t k = some && competes ? key[b] : 0u;
-            eq = some && competes && k == cut;
-            return competes ? (some ? k > cut : take > 0) : b <= own;
-        };
-        const int chunks = own / 64 + 1;   // of 64 blocks
-        if constexpr (TEAM == 1) {
-            int done = 0;
-            for (int ch = 0; ch < chunks && done < a.n_blocks; ++ch) {
-                bool eq;
-                bool sel = taken(ch * 64 + lane, eq);
-                const unsigned long long eqs = __builtin_amdgcn_ballot_w64(eq);
-                if (eq) sel = __popcll(eqs & below) < equals;
-                equals -= min(equals, (int)__popcll(eqs));
-                const unsigned long long sels = __builtin_amdgcn_ballot_w64(sel);
-                const int at = done + (int)__popcll(sels & below);
-                if (sel && at < a.n_blocks) out[at] = ch * 64 + lane;
-                done += (int)__popcll(sels);
-            }
-            for (int i = min(done, a.n_blocks) + lane; i < a.n_blocks; i += 64) out[i] = -1;
-        } else {
-            for (int ch = wave; ch < chunks; ch += TEAM) {
-                bool eq;
-                const bool sel = taken(ch * 64 + lane, eq);
-                const uint32_t more = (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(sel)), equal = (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(eq));
-                if (lane == 0) {
-                    chunk_more[ch] = more;
-                    chunk_equal[ch] = equal;
-                }
-            }
-            __syncthreads();
-            for (int ch = wave; ch < chunks; ch += TEAM) {
-                int more = 0, equal = 0;   // in the chunks before this one
-                for (int i = lane; i < ch; i += 64) {
-                    more += (int)chunk_more[i];
-                    equal += (int)chunk_equal[i];
-                }
-                more = of_wave(more, sum_of());
-                equal = of_wave(equal, sum_of());
-                bool eq;
-                bool sel = taken(ch * 64 + lane, eq);
-                if (eq) sel = equal + (int)__popcll(__builtin_amdgcn_ballot_w64(eq) & below) < equals;
-                const unsigned long long sels = __builtin_amdgcn_ballot_w64(sel);
-                const int at = more + min(equal, equals) + (int)__popcll(sels & below);
-                if (sel && at < a.n_blocks) out[at] = ch * 64 + lane;
-            }
-            const int all = min(a.n_blocks, own + 1);
-            for (int i = all + (int)threadIdx.x; i < a.n_blocks; i += 64 * TEAM) out[i] = -1;
-        }
-    }
+    for (int t = TEAM == 1 ? wave : 0; t < nt; t += TEAMS)
+        pick_blocks<TEAM>(keys + t * a.blocks - s0, (rq.P + t0 + t) / 64, a.n_blocks, a.n_first, a.n_last, team_sh[TEAM == 1 ? wave : 0], chunk_more, chunk_equal,
+                          a.chosen + ((size_t)(rq.row0 + t0 + t) * a.hkv + h) * a.n_blocks);
 }

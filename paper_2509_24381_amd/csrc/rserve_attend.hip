@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "attend_few.h"
+#include "attend_selected.h"
 #include "attention.h"
 #include "block_select.h"
 #include "host_state.h"
@@ -878,7 +879,6 @@ rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int*
         for (int i = 0; i < R; ++i)
             if (lens[i] > 0) kvs[i]->bounded[layer] = kvs[i]->len[layer] / 64;
     }
-    // the attention kernel's table, copied by the first selection launch
     std::vector<FewRequest> reqs;
     int row = 0;
     for (int i = 0; i < R; ++i) {
@@ -898,48 +898,110 @@ rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int*
         else while (2 * parts * units <= places && 2 * parts <= apart) parts *= 2;
     }
     if ((size_t)units * parts * rbn > SLOT_ROWS / 16) parts = 1;
+    const bool wide = (size_t)units <= SELECT_WIDE_UNITS;
+    int halvings = 0;
+    for (int x = 1; x < ctx->group; x *= 2) ++halvings;
+    const size_t few_words = few_table_words(reqs), few_pages = few_table_pages(kvs, reqs), selected_words = few_words + BOUNDS_WORDS * reqs.size();
+    const int split = wide ? std::min((longest + SELECT_ROUND - 1) / SELECT_ROUND, std::max(1, 2 * ctx->n_cu / units)) : 1;
+    // One kernel selects and attends where the descriptors fit its arguments and the keys of scores its LDS (page numbers may be in place); where scores
+    // are a launch of their own, only with so many tokens that a workgroup of 16 wavefronts for each selection is no faster.  us a pass, kernels of their own /
+    // one, 4 KV heads: lists of 8 on 16000, one token 15.4 / 12.2, 64 tokens 17.5 / 12.7; of 32, one 17.1 / 15.2, 64 27.2 / 22.0; on 3000, 64
+    // tokens, lists of 16 17.8 / 14.1; on 100000, lists of 32, one 21.8 / 22.9, 16 29.5 / 29.8, 32 37.6 / 35.4, 48 42.5 / 43.2, 64 45.7 / 41.5.
+    const bool selected = wide && longest <= SELECTED_BLOCKS && selected_words <= TABLE_WORDS && (split == 1 || 2 * units >= ctx->n_cu);
+    const bool in_arguments = selected && selected_words + few_pages <= TABLE_WORDS;
     int slot = 0;
-    if ((s = ring_acquire(ctx, st, &slot)) != RS_OK) return s;
-    uint32_t* const table = reinterpret_cast<uint32_t*>(ctx->pinned[slot]);
-    write_few_table(ctx, layer, kvs, reqs, true, table, table + few_table_words(reqs));
-    const int copy_chunks = (int)(align_up((few_table_words(reqs) + few_table_pages(kvs, reqs)) * 4, 16) / 16);
-    int* const list = chosen ? chosen : reinterpret_cast<int*>(ws + L.chosen_at);
+    if (!in_arguments && (s = ring_acquire(ctx, st, &slot)) != RS_OK) return s;
+    uint32_t* const stage = in_arguments ? nullptr : reinterpret_cast<uint32_t*>(ctx->pinned[slot]);
 
     SelectArgs sa{};
     sa.hkv = f.n_kv_heads; sa.g = ctx->group;
-    for (int x = 1; x < ctx->group; x *= 2) ++sa.halvings;
+    sa.halvings = halvings;
     sa.q = (const bf16*)q; sa.ld_q = ld_q;
     sa.blocks = (int)align_up(longest, 4);
     sa.n_blocks = n_blocks; sa.n_first = n_first; sa.n_last = n_last;
-    sa.chosen = list;
-    const bool wide = (size_t)units <= SELECT_WIDE_UNITS;
     sa.tokens = wide ? 1 : (int)std::min<size_t>(4, SELECT_LDS / ((size_t)longest * 4));
-    sa.copy_from = reinterpret_cast<const uint4*>(ctx->pinned_dev[slot]);
-    sa.copy_to = reinterpret_cast<uint4*>(ws);
-    sa.copy_chunks = copy_chunks;
-    sa.split = wide ? std::min((longest + SELECT_ROUND - 1) / SELECT_ROUND, std::max(1, 2 * ctx->n_cu / units)) : 1;
+    sa.split = split;
     sa.shared_keys = reinterpret_cast<uint32_t*>(ws + L.keys_at);
-    constexpr int threads = 256;
-    constexpr int WINDOW = TABLE_WORDS / 20;   // requests whose descriptors the kernel arguments hold
-    for (size_t i0 = 0; i0 < reqs.size(); i0 += WINDOW) {
-        const int n = (int)std::min<size_t>(WINDOW, reqs.size() - i0);
-        InlineTable tab;
+    FewArgs a{};
+    a.n_req = (int)reqs.size();
+    a.hkv = f.n_kv_heads; a.g = ctx->group;
+    a.q = (const bf16*)q; a.ld_q = ld_q; a.out = (bf16*)out; a.ld_out = ld_out;
+    a.scale_log2e = (float)(1.4426950408889634 * (double)scale);
+    a.slots = reinterpret_cast<float*>(ws + L.slots_at);
+    a.n_blocks = n_blocks;
+    a.list_parts = parts;
+
+    const auto bounds_at = [&](const FewRequest& r) {
+        const rs_kv* kv = kvs[r.kv];
+        const size_t plane = (size_t)layer * f.n_kv_heads * kv->bound_blocks;
+        return BoundsAt{(uint64_t)(uintptr_t)(kv->bound_codes + plane * 2 * f.head_dim), (uint64_t)(uintptr_t)(kv->bound_units + plane), kv->bound_blocks, 0};
+    };
+    // the selection's descriptors of n requests from the i0-th on; their groups of tokens
+    const auto write_select_table = [&](size_t i0, int n, InlineTable& tab) {
         uint32_t groups = 0;
         for (int j = 0; j < n; ++j) {
             const FewRequest& r = reqs[i0 + j];
-            const rs_kv* kv = kvs[r.kv];
-            const size_t plane = (size_t)layer * f.n_kv_heads * kv->bound_blocks;
+            const BoundsAt at = bounds_at(r);
             SelectReq sr{};
-            sr.codes = (uint64_t)(uintptr_t)(kv->bound_codes + plane * 2 * f.head_dim);
-            sr.units = (uint64_t)(uintptr_t)(kv->bound_units + plane);
-            sr.room = kv->bound_blocks;
-            sr.row0 = r.row0; sr.T = r.T; sr.P = kv->len[layer] - r.T;
+            sr.codes = at.codes; sr.units = at.units; sr.room = at.room;
+            sr.row0 = r.row0; sr.T = r.T; sr.P = kvs[r.kv]->len[layer] - r.T;
             tab.w[j] = groups;
             memcpy(&tab.w[table_reqs_at(n) + 16 * j], &sr, sizeof(sr));
             groups += (uint32_t)((r.T + sa.tokens - 1) / sa.tokens);
         }
+        return groups;
+    };
+    constexpr int threads = 256;
+    if (selected) {
+        const int n = a.n_req;
+        if (sa.split > 1) {   // scores first, several workgroups per token
+            InlineTable tab;
+            const uint32_t groups = write_select_table(0, n, tab) * sa.split;
+            sa.n_req = n;
+            sa.groups = (int)groups;
+            with_table(tab, (size_t)table_reqs_at(n) + 16 * n, [&](const auto& table) {
+                typedef std::decay_t<decltype(table)> Tab;
+                const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(groups, f.n_kv_heads), dim3(threads), 0, st, sa, table); };
+                if (f.head_dim == 128) launch(block_select_kernel<128, true, SELECT_SCORES, Tab>);
+                else launch(block_select_kernel<64, true, SELECT_SCORES, Tab>);
+            });
+            RS_HIP(hipGetLastError());
+        }
+        InlineTable tab;
+        write_few_table(ctx, layer, kvs, reqs, true, tab.w, in_arguments ? tab.w + selected_words : stage);
+        for (int j = 0; j < n; ++j) {
+            const BoundsAt at = bounds_at(reqs[j]);
+            memcpy(&tab.w[few_words + BOUNDS_WORDS * j], &at, sizeof(at));
+        }
+        if (!in_arguments) a.pages = reinterpret_cast<const uint32_t*>(ctx->pinned_dev[slot]);
+        SelectedArgs se{halvings, n_first, n_last, sa.blocks, sa.shared_keys, chosen};
+        with_table(tab, selected_words + (in_arguments ? few_pages : 0), [&](const auto& table) {
+            typedef std::decay_t<decltype(table)> Tab;
+            for_kind(ctx, fp8, [&](auto d, auto f8) {
+                constexpr int D = decltype(d)::value;
+                constexpr bool FP8 = decltype(f8)::value;
+                const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(units * parts), dim3(64 * FEW_WAVES), 0, st, a, se, table); };
+                if (sa.split > 1) launch(attend_selected_kernel<D, FP8, true, Tab>);
+                else launch(attend_selected_kernel<D, FP8, false, Tab>);
+                if (parts > 1) hipLaunchKernelGGL((few_merge_kernel<D, true, Tab>), dim3(units * rbn, D / 32), dim3(256), 0, st, a, table);
+            });
+        });
+        RS_HIP(hipGetLastError());
+        return in_arguments ? RS_OK : ring_commit(ctx, st);
+    }
+    // the attention kernel's table, copied by the first selection launch
+    write_few_table(ctx, layer, kvs, reqs, true, stage, stage + few_words);
+    sa.chosen = chosen ? chosen : reinterpret_cast<int*>(ws + L.chosen_at);
+    sa.copy_from = reinterpret_cast<const uint4*>(ctx->pinned_dev[slot]);
+    sa.copy_to = reinterpret_cast<uint4*>(ws);
+    sa.copy_chunks = (int)(align_up((few_words + few_pages) * 4, 16) / 16);
+    constexpr int WINDOW = TABLE_WORDS / 20;   // requests whose descriptors the kernel arguments hold
+    for (size_t i0 = 0; i0 < reqs.size(); i0 += WINDOW) {
+        const int n = (int)std::min<size_t>(WINDOW, reqs.size() - i0);
+        InlineTable tab;
+        const uint32_t groups = write_select_table(i0, n, tab);
         sa.n_req = n;
-        const unsigned copying = i0 == 0 ? (unsigned)((copy_chunks + threads - 1) / threads) : 0u;
+        const unsigned copying = i0 == 0 ? (unsigned)((sa.copy_chunks + threads - 1) / threads) : 0u;
         const size_t lds = (size_t)sa.tokens * sa.blocks * 4;
         const auto select = [&](auto d) {
             constexpr int D = decltype(d)::value;
@@ -961,16 +1023,8 @@ rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int*
         RS_HIP(hipGetLastError());
         if (i0 == 0 && (s = ring_commit(ctx, st)) != RS_OK) return s;
     }
-    FewArgs a{};
     a.table = reinterpret_cast<const uint32_t*>(ws);
-    a.n_req = (int)reqs.size();
-    a.hkv = f.n_kv_heads; a.g = ctx->group;
-    a.q = (const bf16*)q; a.ld_q = ld_q; a.out = (bf16*)out; a.ld_out = ld_out;
-    a.scale_log2e = (float)(1.4426950408889634 * (double)scale);
-    a.slots = reinterpret_cast<float*>(ws + L.slots_at);
-    a.chosen = list;
-    a.n_blocks = n_blocks;
-    a.list_parts = parts;
+    a.chosen = sa.chosen;
     return launch_few<true>(ctx, fp8, false, a, (uint32_t)(units * parts), (uint32_t)(units * rbn), parts > 1, NoTable{}, st);
 } catch (const std::exception& e) {
     return not_allocated(e);
