@@ -903,11 +903,12 @@ rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int*
     for (int x = 1; x < ctx->group; x *= 2) ++halvings;
     const size_t few_words = few_table_words(reqs), few_pages = few_table_pages(kvs, reqs), selected_words = few_words + BOUNDS_WORDS * reqs.size();
     const int split = wide ? std::min((longest + SELECT_ROUND - 1) / SELECT_ROUND, std::max(1, 2 * ctx->n_cu / units)) : 1;
-    // One kernel selects and attends where the descriptors fit its arguments and the keys of scores its LDS (page numbers may be in place); where scores
-    // are a launch of their own, only with so many tokens that a workgroup of 16 wavefronts for each selection is no faster.  us a pass, kernels of their own /
-    // one, 4 KV heads: lists of 8 on 16000, one token 15.4 / 12.2, 64 tokens 17.5 / 12.7; of 32, one 17.1 / 15.2, 64 27.2 / 22.0; on 3000, 64
-    // tokens, lists of 16 17.8 / 14.1; on 100000, lists of 32, one 21.8 / 22.9, 16 29.5 / 29.8, 32 37.6 / 35.4, 48 42.5 / 43.2, 64 45.7 / 41.5.
-    const bool selected = wide && longest <= SELECTED_BLOCKS && selected_words <= TABLE_WORDS && (split == 1 || 2 * units >= ctx->n_cu);
+    // One kernel selects and attends where the descriptors fit its arguments and the keys of scores its LDS (page numbers may be in place), as long as
+    // all its workgroups run at once; where scores are a launch of their own, only with so many tokens that a workgroup of 16 wavefronts for
+    // each selection is no faster.  us a pass, kernels of their own / one, 4 KV heads: lists of 8 on 16000, one token 15.4 / 12.2, 64 tokens
+    // 17.5 / 12.7, 128 19.4 / 16.6, 256 27.1 / 27.3, 500 38.6 / 45.1; of 32, one 17.1 / 15.2, 64 27.2 / 22.0, 128 33.9 / 30.4, 256 54.0 / 53.2, 500
+    // 91.9 / 95.8; on 50000, of 32, 128 45.2 / 40.9, 256 72.9 / 77.0; on 100000, of 32, one 21.8 / 22.9, 16 29.5 / 29.8, 32 37.6 / 35.4, 64 45.7 / 41.5.
+    const bool selected = units <= FEW_PLACES * ctx->n_cu && longest <= SELECTED_BLOCKS && selected_words <= TABLE_WORDS && (split == 1 || 2 * units >= ctx->n_cu);
     const bool in_arguments = selected && selected_words + few_pages <= TABLE_WORDS;
     int slot = 0;
     if (!in_arguments && (s = ring_acquire(ctx, st, &slot)) != RS_OK) return s;
