@@ -192,3 +192,18 @@ def test_out_may_be_q(rule, monkeypatch):
     ctx.attend_blocks(0, kvs, lens, q, out, ws, 20)
     ctx.attend_blocks(0, kvs, lens, over, over, ws, 20)
     assert torch.equal(out, over)
+
+
+@pytest.mark.parametrize("kind", ["contiguous", "paged_fp8"])
+@pytest.mark.parametrize("held, rows, n_blocks", [(17000, 70, 6), (17000, 129, 19), (40000, 1, 33), (1100, 300, 5), (3000, 260, 24), (17000, 260, 4)])
+def test_every_way_to_select(kind, held, rows, n_blocks):
+    """Selection and attention in one kernel, with scores taken ahead and without, and in kernels of their own for few tokens and for many."""
+    ctx = T.context(4, 2, 64)
+    kvs, content, g = filled(ctx, kind, [held], 69)
+    kvs[0].new_bounds(held + 64)
+    q = T.normal(g, rows, 256, std=1.5)
+    out, chosen = T.run_blocks(ctx, kvs, [rows], q, n_blocks, 1, 2)
+    T.check_blocks(ctx, kind, [held], [rows], content, q, out, chosen, n_blocks, 1, 2)
+    over = torch.empty_like(out)
+    ctx.attend_blocks(0, kvs, [rows], q, over, ctx.attend_workspace(rows, 1, n_blocks=n_blocks), n_blocks)   # (the lists are not wanted)
+    assert torch.equal(out, over)
