@@ -5,7 +5,8 @@
 
 // One workgroup per (row, part of its list, KV head).  It scores the blocks (or takes the scores that a launch before left, where blocks are
 // many: SCORED) and picks the list, every part for itself, with the four wavefronts that then attend to the part.  Keys of scores lie
-// where the tiles go afterwards.
+// where the tiles go afterwards.  Bound by latency: from queries to codes, scores, digits, list, keys, values; us a pass, one token on 16000, lists
+// of 8 blocks, 12.2 (two kernels 15.4), lists of 32 and the merge 15.2 (17.1); the rule that chooses has more.
 constexpr int SELECTED_BLOCKS = 4096;      // of a cache, at most
 constexpr int SELECTED_LIST = 1024;        // of a list, at most
 struct BoundsAt {                          // of a request: six words of the table, behind the FewReqs

@@ -108,6 +108,7 @@ __global__ __launch_bounds__(256) void key_bounds_kernel(int n_req, int hkv, int
 //     score[block] = unit sum_d (p_d high_d - n_d low_d),  p and n the heads' positive and negative codes, summed: whole numbers, one product
 //  3. a team per token finds the score that the last selected block has, digit by digit of the keys' range (a histogram in LDS per
 //     digit: integers, in any order the same), and writes the blocks down in ascending order.
+// These are the kernels for many tokens, many requests and very long caches; otherwise attend_selected_kernel takes the same steps itself.
 // With many tokens a workgroup has four, a wavefront each, and takes all three steps.  With few (WIDE) it has one, and where that has more
 // blocks than a workgroup scores at once, the first two steps are a launch of their own, of a workgroup per 256 blocks: a compute unit alone
 // gets 33 bytes per ns, 16 us for the bounds of 2046 blocks.  (One launch, the last workgroup to finish selecting: the fence that makes

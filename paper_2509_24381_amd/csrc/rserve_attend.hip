@@ -245,8 +245,8 @@ size_t expansion_bytes(const rs_ctx* c, long tokens) { return (size_t)2 * align_
 // all four wavefronts need every tile it takes 2 and 3 times as long (wavefronts of 32 rows: 1.5 and 2), and parts are that much shorter (us a
 // pass, all alike -> so: 30 single tokens on up to 8000 beside 4 requests of 5 on 3000, 64 query heads, 8 KV heads, 142.7 -> 115.5, 8 bits
 // 91.3 -> 55.8; 24 requests of 3 on up to 6000 beside one of 12 on 5000 68.4 -> 53.4; one of 4 on 8000, alone, 15.8 -> 17.2).
-// us a pass, parts of 4 / 8 / 16 / 24 / 48 tiles, and with this estimate's: 64 requests on up to 8000 tokens 97.4 / 93.2 / 86.0 / 86.6 / 89.0, 88.3; 16 on up to 32000, 8 bits,
-// 73.2 / 68.6 / 66.1 / 64.6 / 59.4, 60.2; 24 of 3 tokens on up to 6000 and one of 12, 64 and 8 heads, 79.6 / 69.5 / 58.3 / 56.6 / 67.0, 54.3.
+// us a pass, parts of 4 / 8 / 16 / 24 / 48 tiles, and with this estimate's: 64 requests on up to 8000 tokens 97.4 / 93.2 / 86.0 / 86.6 / 89.0,
+// 88.3; 16 on up to 32000, 8 bits, 73.2 / 68.6 / 66.1 / 64.6 / 59.4, 60.2; 24 of 3 tokens on up to 6000 and one of 12, 64 and 8 heads, 79.6 / 69.5 / 58.3 / 56.6 / 67.0, 54.3.
 struct FewRequest {
     int kv, row0, T;       // index into kvs, first row, rows
     int units, tiles;      // items per part, tiles
