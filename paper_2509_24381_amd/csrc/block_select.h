@@ -350,20 +350,23 @@ RS_DEVICE void pick_blocks(const uint32_t* key, int own, int n_blocks, int n_fir
             }
         }
         __syncthreads();
-        for (int ch = wave; ch < chunks; ch += TEAM) {
-            int more = 0, equal = 0;   // in the chunks before this one
-            for (int i = lane; i < ch; i += 64) {
-                more += (int)chunk_more[i];
-                equal += (int)chunk_equal[i];
+        uint32_t more_before = 0, equal_before = 0;   // in the chunks before these 64
+        for (int c0 = 0; c0 < chunks; c0 += 64) {
+            const bool there = c0 + lane < chunks;
+            const uint32_t more_from = sum_from_lane(there ? chunk_more[c0 + lane] : 0u), equal_from = sum_from_lane(there ? chunk_equal[c0 + lane] : 0u);
+            const uint32_t more_end = more_before + __builtin_amdgcn_readlane(more_from, 0), equal_end = equal_before + __builtin_amdgcn_readlane(equal_from, 0);
+            for (int ch = c0 + wave; ch < min(chunks, c0 + 64); ch += TEAM) {
+                const int more = (int)(more_end - __builtin_amdgcn_readlane(more_from, ch - c0)), equal = (int)(equal_end - __builtin_amdgcn_readlane(equal_from, ch - c0));
+                bool eq;
+                bool sel = taken(ch * 64 + lane, eq);
+                const unsigned long long eqs = __builtin_amdgcn_ballot_w64(eq);
+                if (eq) sel = equal + (int)__popcll(eqs & below) < equals;
+                const unsigned long long sels = __builtin_amdgcn_ballot_w64(sel);
+                const int at = more + min(equal, equals) + (int)__popcll(sels & below);
+                if (sel && at < n_blocks) out[at] = ch * 64 + lane;
             }
-            more = of_wave(more, sum_of());
-            equal = of_wave(equal, sum_of());
-            bool eq;
-            bool sel = taken(ch * 64 + lane, eq);
-            if (eq) sel = equal + (int)__popcll(__builtin_amdgcn_ballot_w64(eq) & below) < equals;
-            const unsigned long long sels = __builtin_amdgcn_ballot_w64(sel);
-            const int at = more + min(equal, equals) + (int)__popcll(sels & below);
-            if (sel && at < n_blocks) out[at] = ch * 64 + lane;
+            more_before = more_end;
+            equal_before = equal_end;
         }
         const int all = min(n_blocks, own + 1);
         for (int i = all + (int)threadIdx.x; i < n_blocks; i += 64 * TEAM) out[i] = -1;

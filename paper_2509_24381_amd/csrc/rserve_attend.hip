@@ -56,6 +56,7 @@ constexpr size_t SLOT_ROWS = 65536;   // rows there is room for in the slots of 
 // Tokens times KV heads up to which a workgroup selects for one token, and several share its blocks; beyond, for four.  us a pass, four / one, 4 KV
 // heads: 16 tokens on 8000 20.2 / 19.3, on 60000 34.7 / 27.3; 64 on 16000 29.2 / 28.7, on 60000 42.1 / 40.4; 96 on 16000 34.8 / 35.5; 128 on 60000 47.6 / 51.7.
 constexpr size_t SELECT_WIDE_UNITS = 256;
+constexpr int SELECTED_IN_PLACE_BLOCKS = 1024, SELECTED_IN_PLACE_UNITS = 32;   // (see rs_attend_blocks)
 constexpr size_t SELECT_LDS = (size_t)SELECT_MAX_BLOCKS * 4;
 
 // ---- checks that all calls share; *rows_out: the sum of lens (null lens: none)
@@ -903,13 +904,16 @@ rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int*
     for (int x = 1; x < ctx->group; x *= 2) ++halvings;
     const size_t few_words = few_table_words(reqs), few_pages = few_table_pages(kvs, reqs), selected_words = few_words + BOUNDS_WORDS * reqs.size();
     const int split = wide ? std::min((longest + SELECT_ROUND - 1) / SELECT_ROUND, std::max(1, 2 * ctx->n_cu / units)) : 1;
-    // One kernel selects and attends where the descriptors fit its arguments and the keys of scores its LDS (page numbers may be in place), as long as
-    // all its workgroups run at once; where scores are a launch of their own, only with so many tokens that a workgroup of 16 wavefronts for
-    // each selection is no faster.  us a pass, kernels of their own / one, 4 KV heads: lists of 8 on 16000, one token 15.4 / 12.2, 64 tokens
-    // 17.5 / 12.7, 128 19.4 / 16.6, 256 27.1 / 27.3, 500 38.6 / 45.1; of 32, one 17.1 / 15.2, 64 27.2 / 22.0, 128 33.9 / 30.4, 256 54.0 / 53.2, 500
-    // 91.9 / 95.8; on 50000, of 32, 128 45.2 / 40.9, 256 72.9 / 77.0; on 100000, of 32, one 21.8 / 22.9, 16 29.5 / 29.8, 32 37.6 / 35.4, 64 45.7 / 41.5.
-    const bool selected = units <= FEW_PLACES * ctx->n_cu && longest <= SELECTED_BLOCKS && selected_words <= TABLE_WORDS && (split == 1 || 2 * units >= ctx->n_cu);
-    const bool in_arguments = selected && selected_words + few_pages <= TABLE_WORDS;
+    // One kernel selects and attends where the descriptors fit its arguments and the keys of scores its LDS, as long as all its workgroups run at
+    // once.  Page numbers are beside the descriptors or in place; a token or two whose scores are a launch of their own and whose pages
+    // are many have theirs copied behind the scores instead, for kernels of their own.  us a pass, kernels of their own / one, 4 KV heads: lists of 8
+    // on 16000, one token 15.4 / 12.2, 64 tokens 17.5 / 12.7, 128 19.4 / 16.6, 256 27.1 / 27.3, 500 38.6 / 45.1; of 32, one 17.1 / 15.2, 64 27.2 / 22.0,
+    // 256 54.0 / 53.2, 500 91.9 / 95.8; on 60000, of 8, one 19.0 / 17.7, 16 21.3 / 18.4, of 32, one 21.5 / 20.5; on 130000, of 32, one 22.3 / 23.2, 4
+    // 23.1 / 23.7, 8 25.5 / 24.4, 64 46.8 / 46.3; contiguous, 8 bits, one 22.1 / 21.2, 8 24.9 / 22.3.
+    const bool fits = selected_words + few_pages <= TABLE_WORDS;
+    const bool selected = units <= FEW_PLACES * ctx->n_cu && longest <= SELECTED_BLOCKS && selected_words <= TABLE_WORDS &&
+                          (split == 1 || fits || longest <= SELECTED_IN_PLACE_BLOCKS || units >= SELECTED_IN_PLACE_UNITS);
+    const bool in_arguments = selected && fits;
     int slot = 0;
     if (!in_arguments && (s = ring_acquire(ctx, st, &slot)) != RS_OK) return s;
     uint32_t* const stage = in_arguments ? nullptr : reinterpret_cast<uint32_t*>(ctx->pinned[slot]);
@@ -955,19 +959,6 @@ rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int*
     constexpr int threads = 256;
     if (selected) {
         const int n = a.n_req;
-        if (sa.split > 1) {   // scores first, several workgroups per token
-            InlineTable tab;
-            const uint32_t groups = write_select_table(0, n, tab) * sa.split;
-            sa.n_req = n;
-            sa.groups = (int)groups;
-            with_table(tab, (size_t)table_reqs_at(n) + 16 * n, [&](const auto& table) {
-                typedef std::decay_t<decltype(table)> Tab;
-                const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(groups, f.n_kv_heads), dim3(threads), 0, st, sa, table); };
-                if (f.head_dim == 128) launch(block_select_kernel<128, true, SELECT_SCORES, Tab>);
-                else launch(block_select_kernel<64, true, SELECT_SCORES, Tab>);
-            });
-            RS_HIP(hipGetLastError());
-        }
         InlineTable tab;
         write_few_table(ctx, layer, kvs, reqs, true, tab.w, in_arguments ? tab.w + selected_words : stage);
         for (int j = 0; j < n; ++j) {
@@ -975,6 +966,19 @@ rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int*
             memcpy(&tab.w[few_words + BOUNDS_WORDS * j], &at, sizeof(at));
         }
         if (!in_arguments) a.pages = reinterpret_cast<const uint32_t*>(ctx->pinned_dev[slot]);
+        if (sa.split > 1) {   // scores first, several workgroups per token
+            InlineTable select_tab;
+            const uint32_t groups = write_select_table(0, n, select_tab) * sa.split;
+            sa.n_req = n;
+            sa.groups = (int)groups;
+            with_table(select_tab, (size_t)table_reqs_at(n) + 16 * n, [&](const auto& table) {
+                typedef std::decay_t<decltype(table)> Tab;
+                const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(groups, f.n_kv_heads), dim3(threads), 0, st, sa, table); };
+                if (f.head_dim == 128) launch(block_select_kernel<128, true, SELECT_SCORES, Tab>);
+                else launch(block_select_kernel<64, true, SELECT_SCORES, Tab>);
+            });
+            RS_HIP(hipGetLastError());
+        }
         SelectedArgs se{halvings, n_first, n_last, sa.blocks, sa.shared_keys, chosen};
         with_table(tab, selected_words + (in_arguments ? few_pages : 0), [&](const auto& table) {
             typedef std::decay_t<decltype(table)> Tab;
