@@ -207,3 +207,16 @@ def test_every_way_to_select(kind, held, rows, n_blocks):
     over = torch.empty_like(out)
     ctx.attend_blocks(0, kvs, [rows], q, over, ctx.attend_workspace(rows, 1, n_blocks=n_blocks), n_blocks)   # (the lists are not wanted)
     assert torch.equal(out, over)
+
+
+@pytest.mark.parametrize("kind", ["paged", "paged_fp8"])
+@pytest.mark.parametrize("rows, n_blocks", [(1, 9), (3, 40), (16, 9)])
+def test_selection_from_many_pages(kind, rows, n_blocks):
+    """More pages than the kernel arguments hold: a token or two select in a kernel of their own, more in the one that attends."""
+    held = 70000
+    ctx = T.context(4, 2, 64, max_pos=80000)
+    kvs, content, g = filled(ctx, kind, [held], 70)
+    kvs[0].new_bounds(held + 64)
+    q = T.normal(g, rows, 256, std=1.5)
+    out, chosen = T.run_blocks(ctx, kvs, [rows], q, n_blocks, 1, 2)
+    T.check_blocks(ctx, kind, [held], [rows], content, q, out, chosen, n_blocks, 1, 2)
