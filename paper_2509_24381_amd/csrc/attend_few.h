@@ -74,6 +74,7 @@ RS_DEVICE const uint32_t* table_of(const Tab& tab, const uint32_t* device_table)
 }
 // The last request whose first item is at most `id`.
 RS_DEVICE int request_of(const uint32_t* table, int n_req, uint32_t id) {
+    if (n_req == 1) return 0;
     const int lane = threadIdx.x & 63;
     int at = -1;
     for (int i0 = 0; i0 < n_req; i0 += 64) {
