@@ -1,7 +1,7 @@
 // Attention of few query rows per KV head: the tokens a request generates one at a time, a few drafted ones, or - with a
 // list of blocks per token - any tokens that attend to selected blocks only.
 //
-//   out[row] = sum_k w_k value_k / sum_k w_k,   w_k = 2^(scale log2e q . key_k - m),  m a reference that tracks the maximum
+//   out[row] = sum_k w_k value_k / sum_k w_k,   w_k = 2^(scale log2e (q . key_k - m)),  m a reference that tracks the maximum
 //
 // Bound by the bytes of the keys and values: a tile of 64 keys is 32 KB (d = 128, bfloat16), and the rows that share it - the g
 // query heads of a KV head, times the tokens - give it 16 MFMAs of 16 clocks per 16 rows and product.  So wavefronts share no tiles: each
@@ -16,7 +16,10 @@
 // and the assignment of MFMA rows to keys is chosen so that the four scores a lane holds of each of its sub-tiles are, put together, the
 // consecutive keys that it has to feed to the second product.  8-bit tiles are loaded 16 codes at a time (the keys' order
 // changes with it) and become bfloat16, exactly, in registers; their scales go into the softmax's scale and the output.
-// Scores, references, row sums and output sums are fp32.  A weight becomes bfloat16 for the second product, whose operands have 16 bits; the row
+// Scores, references, row sums and output sums are fp32.  References are scores as the products leave them, and a weight's exponent is their
+// difference times the scale: zero, exactly, for the key that is the reference.  (With the scale in the reference, whose rounding an fma does not
+// repeat, all weights of a row move by that rounding, and from scores of 2^32 on out of fp32's range.)
+//  A weight becomes bfloat16 for the second product, whose operands have 16 bits; the row
 // sum takes it before that.  The output is rounded once.  A masked key has weight zero; where its value is an infinity or NaN the row
 // comes out not finite and is done again by exact_row, which leaves masked values alone.
 //
@@ -360,11 +363,11 @@ RS_DEVICE void attend_rows(const FewArgs& a, const FewReq& rq, const uint32_t* p
             for (int t = 0; t < 4; ++t)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[b][t][e]);
-            mx = of_quarters(mx, larger_of()) * sc;
-            const bool move = mx > m[b] + FEW_HEADROOM;   // (at first m is minus infinity)
+            mx = of_quarters(mx, larger_of());
+            const bool move = (mx - m[b]) * sc > FEW_HEADROOM;   // (at first m is minus infinity)
             if (__builtin_amdgcn_ballot_w64(move)) {
                 const float m_new = move ? mx : m[b];
-                const float alpha = m[b] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[b] - m_new);
+                const float alpha = m[b] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m[b] - m_new) * sc);
                 m[b] = m_new;
                 l[b] *= alpha;
 #pragma unroll
@@ -377,7 +380,7 @@ RS_DEVICE void attend_rows(const FewArgs& a, const FewReq& rq, const uint32_t* p
             for (int t = 0; t < 4; ++t)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][t][e], sc, -ref));
+                    const float p = __builtin_amdgcn_exp2f((s[b][t][e] - ref) * sc);
                     l[b] += p;
                     pf[b][t >> 1][(t & 1) * 4 + e] = f32_to_bf16(p);
                 }
@@ -429,7 +432,7 @@ RS_DEVICE void attend_rows(const FewArgs& a, const FewReq& rq, const uint32_t* p
         __syncthreads();
         float big = m_own;
         for (int w = set; w < FEW_WAVES; w += sets) big = fmaxf(big, m_sh[w][r]);
-        const float weight = m_own == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_own - big);
+        const float weight = m_own == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m_own - big) * sc);
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
             f32x4 o = acc[own_block][dt];
@@ -444,7 +447,7 @@ RS_DEVICE void attend_rows(const FewArgs& a, const FewReq& rq, const uint32_t* p
             float M = -INFINITY, L = 0.0f, o[PER] = {};
             for (int w = sb; w < FEW_WAVES; w += sets) M = fmaxf(M, m_sh[w][row]);
             for (int w = sb; w < FEW_WAVES; w += sets) {
-                L += l_sh[w][row] == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(m_sh[w][row] - M) * l_sh[w][row];
+                L += l_sh[w][row] == 0.0f ? 0.0f : __builtin_amdgcn_exp2f((m_sh[w][row] - M) * sc) * l_sh[w][row];
 #pragma unroll
                 for (int j = 0; j < PER; ++j) o[j] += sums_of(w, row)[f0 + j];
             }
@@ -545,7 +548,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
     attend_rows<D, FP8, LIST, RB>(a, rq, pages, rows, part, parts, unit, n, list, lds, m_sh, l_sh);
 }
 
-// Joins the parts of 16 rows:  M = max_p m_p,  out = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p.  One workgroup per 16 rows and 32
+// Joins the parts of 16 rows:  M = max_p m_p,  out = sum_p 2^(c (m_p - M)) O_p / sum_p 2^(c (m_p - M)) l_p, c the scale.  One workgroup per 16 rows and 32
 // features, a quarter of the parts per 64 threads (16 rows x 4 chunks of 8 features).  3 to 5 us, the latency of a launch and of loads that
 // follow one another.  (Joining in the kernel before, by the last workgroup to arrive, needs a fence across the chip: 64 single tokens 84 -> 198 us.)
 template <int D, bool LIST, class Tab>
@@ -587,6 +590,7 @@ __global__ __launch_bounds__(256) void few_merge_kernel(FewArgs a, Tab tab) {
     const int slot_blocks = few_row_blocks(LIST ? a.g : min(rq.T * a.g, FEW_GROUP));
     const float* const base = a.slots + (size_t)(rq.slot0 + unit * parts * slot_blocks + b) * FewSlot<D>::FLOATS;
     const size_t next = (size_t)slot_blocks * FewSlot<D>::FLOATS;
+    const float sc = a.scale_log2e * rq.k_scale;   // (bfloat16 caches: times one)
     // four parts at a time, all their loads in flight together, on to a running reference M
     float M = -INFINITY, L = 0.0f, o[8] = {};
     for (int p0 = group; p0 < parts; p0 += 16) {
@@ -604,7 +608,7 @@ __global__ __launch_bounds__(256) void few_merge_kernel(FewArgs a, Tab tab) {
 #pragma unroll
         for (int k = 0; k < 4; ++k)
             if (p0 + 4 * k < parts) big = fmaxf(big, mp[k]);
-        const float alpha = M == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(M - big);
+        const float alpha = M == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((M - big) * sc);
         M = big;
         if (L != 0.0f) {   // (sums of nothing stay, whatever the reference)
             L *= alpha;
@@ -614,7 +618,7 @@ __global__ __launch_bounds__(256) void few_merge_kernel(FewArgs a, Tab tab) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             // (a part none of whose keys count has a row sum of zero and no reference)
-            const float w = p0 + 4 * k >= parts || lp[k] == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(mp[k] - M);
+            const float w = p0 + 4 * k >= parts || lp[k] == 0.0f ? 0.0f : __builtin_amdgcn_exp2f((mp[k] - M) * sc);
             if (p0 + 4 * k >= parts) continue;
             L += w * lp[k];
 #pragma unroll
@@ -628,7 +632,7 @@ __global__ __launch_bounds__(256) void few_merge_kernel(FewArgs a, Tab tab) {
     __syncthreads();
     {
         const float big = fmaxf(fmaxf(m_sh[0][row], m_sh[1][row]), fmaxf(m_sh[2][row], m_sh[3][row]));
-        const float w = L == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(M - big);
+        const float w = L == 0.0f ? 0.0f : __builtin_amdgcn_exp2f((M - big) * sc);
         L *= w;
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[e] *= w;

@@ -462,7 +462,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_pipelined_kernel(c
 #pragma unroll
                     for (int j = 0; j < D / 64; ++j) slot[((size_t)((lane >> 2) + 16 * j) * BLOCK_ROWS + rs) * 4 + (lane & 3)] = eo[j];
                     if (lane == 0) {
-                        slot[(size_t)D * BLOCK_ROWS + rs] = fmaxf(em / scale_log2e, -3.402823466e38f);
+                        slot[(size_t)D * BLOCK_ROWS + rs] = fmaxf(em, -3.402823466e38f);
                         slot[(size_t)(D + 1) * BLOCK_ROWS + rs] = el;
                     }
                 } else {

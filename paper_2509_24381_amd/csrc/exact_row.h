@@ -12,7 +12,8 @@ RS_DEVICE float tile_element(global_bytes tile, int i) {
 
 // One query row over tiles [i0, i1), by one wavefront, without the matrix pipe: what the attention kernels fall back on where a row's result is
 // not finite.  A masked value enters their products with weight zero, and zero times an infinity or NaN is NaN; here it does not enter.
-// Returns the reference and row sum, and in o the unnormalised output of features lane + 64 i.
+// Returns the reference (the largest score, as the product leaves it) and the row sum of weights 2^(sc (score - m)), and in o the unnormalised
+// output of features lane + 64 i.
 template <int D, bool FP8, class TileAt>
 RS_DEVICE void exact_row(const bf16* q, float sc, int qpos, int i0, int i1, TileAt&& tile_at, float& m, float& l, float (&o)[D / 64]) {
     const int lane = threadIdx.x & 63;
@@ -28,12 +29,12 @@ RS_DEVICE void exact_row(const bf16* q, float sc, int qpos, int i0, int i1, Tile
         if (live <= 0) continue;
         float s = 0.0f;
         for (int d = 0; d < D; ++d) s = __builtin_fmaf(bf16_to_f32(q[d]), tile_element<FP8>(kt, lane * D + d), s);
-        s = lane < live ? s * sc : -INFINITY;
+        s = lane < live ? s : -INFINITY;
         float mx = s;
 #pragma unroll
         for (int off = 32; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off, WAVE));
         const float m_new = fmaxf(m, mx), ref = m_new == -INFINITY ? 0.0f : m_new;
-        const float p = lane < live ? __builtin_amdgcn_exp2f(s - ref) : 0.0f, alpha = __builtin_amdgcn_exp2f(m - ref);
+        const float p = lane < live ? __builtin_amdgcn_exp2f((s - ref) * sc) : 0.0f, alpha = __builtin_amdgcn_exp2f((m - ref) * sc);
         l = l * alpha + wave_sum(p);
 #pragma unroll
         for (int j = 0; j < D / 64; ++j) o[j] *= alpha;
