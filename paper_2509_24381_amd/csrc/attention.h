@@ -138,7 +138,10 @@ constexpr float ATT_RESCALE_SUM = 256.0f, ATT_HEADROOM_LOG2 = 6.0f;
 
 // ROWS: the output is row-major and final, for a caller instead of the output projection: rows that are not finite are taken again
 // one by one, so that what a query does not see does not reach it (a masked key's weight is zero, but zero times an infinite or
-// NaN value is NaN; the layer has no use for rows behind such a token).
+// NaN value is NaN; the layer has no use for rows behind such a token).  So are rows whose scaled reference is beyond ATT_REF_LIMIT: up to
+// there its rounding and the headroom's stay below 2^-3, and a row's weights are off by a common factor that the row sum cancels; from 2^32 on
+// they would leave fp32's range altogether.
+constexpr float ATT_REF_LIMIT = 1048576.0f;   // 2^20
 template <int D, bool MAY_PAGE, int WAVES, bool ROWS = false>
 __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_pipelined_kernel(const ReqDesc* __restrict__ reqs,
                                                                                 const AttnItem* __restrict__ items,
@@ -437,7 +440,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_pipelined_kernel(c
 
     const float l_tot = l_run + __shfl_xor(l_run, 32, WAVE);
     if constexpr (ROWS) {
-        bool bad = !(fabsf(l_tot) <= 3.402823466e38f);
+        // (each row sees the first key of its part: a sum of nothing is all scores at minus infinity, or weights that flushed)
+        bool bad = !(l_tot > 0.0f && l_tot <= 3.402823466e38f) || !(fabsf(m_ref * scale_log2e) <= ATT_REF_LIMIT);
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
