@@ -286,7 +286,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_pipelined_kernel(c
     f32x16 s0, s1;            // raw scores of the two halves of a tile: register r of half hh holds key
                               // key0 + hh*32 + 16*(r>>3) + 8*half + (r&7)
     bf16x8 pf0[2], pf1[2];    // probabilities of the two halves, as the P.V product wants them
-    const float headroom = ATT_HEADROOM_LOG2 / scale_log2e;   // (raw scores)
+    // (raw scores.  ROWS: any scale there is; the cap, far below fp32's end, only binds where it is below 2^-117)
+    const float headroom = ROWS ? fminf(ATT_HEADROOM_LOG2 / scale_log2e, 1e36f) : ATT_HEADROOM_LOG2 / scale_log2e;
     float m_ref;        // reference of this lane's query, raw scores (shared by both half-waves)
     float l_run = 0.0f; // running sum over THIS half-wave's keys
     const f32x16 zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};

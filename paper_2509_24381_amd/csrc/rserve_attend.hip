@@ -346,6 +346,8 @@ rs_status launch_few(const rs_ctx* ctx, bool fp8, bool pairs, const FewArgs& a, 
     return RS_OK;
 }
 
+float log2e_times(float scale) { return (float)(1.4426950408889634 * (double)scale); }
+
 rs_status check_attend(const rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, int R, const void* q, long ld_q, const void* out, long ld_out,
                        float* scale, long* rows) {
     rs_status s = check_call(ctx, layer, kvs, lens, true, R, rows);
@@ -354,6 +356,12 @@ rs_status check_attend(const rs_ctx* ctx, int layer, rs_kv* const* kvs, const in
         if (lens[i] > kvs[i]->len[layer]) return fail(RS_EINVAL, "lens[%d] = %d exceeds the %d cached tokens", i, lens[i], kvs[i]->len[layer]);
     if (*scale == 0.0f) *scale = (float)(1.0 / std::sqrt((double)ctx->cfg.head_dim));
     if (!(*scale > 0.0f) || !std::isfinite(*scale)) return fail(RS_EINVAL, "scale = %g must be positive and finite, or 0", *scale);
+    // what the kernels multiply by: a masked score, minus infinity, times zero would be NaN, and so would a score of zero times infinity
+    for (int i = 0; i < R; ++i) {
+        const float factor = log2e_times(*scale) * kvs[i]->k_scale;
+        if (!(factor > 0.0f) || !std::isfinite(factor))
+            return fail(RS_EINVAL, "scale = %g times log2 e times the keys' scale %g of kvs[%d] is not a positive number in 32 bits", *scale, kvs[i]->k_scale, i);
+    }
     if (*rows == 0) return RS_OK;
     if ((s = check_matrix("q", q, ld_q, ctx->q_dim)) != RS_OK) return s;
     return check_matrix("out", out, ld_out, ctx->q_dim);
@@ -645,7 +653,7 @@ rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, 
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     if ((s = refuse_capture(st)) != RS_OK) return s;
     char* const ws = reinterpret_cast<char*>(workspace);
-    const float scale_log2e = (float)(1.4426950408889634 * (double)scale);
+    const float scale_log2e = log2e_times(scale);
 
     // ---- requests of few rows
     std::vector<FewRequest> few;
@@ -931,7 +939,7 @@ rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int*
     a.n_req = (int)reqs.size();
     a.hkv = f.n_kv_heads; a.g = ctx->group;
     a.q = (const bf16*)q; a.ld_q = ld_q; a.out = (bf16*)out; a.ld_out = ld_out;
-    a.scale_log2e = (float)(1.4426950408889634 * (double)scale);
+    a.scale_log2e = log2e_times(scale);
     a.slots = reinterpret_cast<float*>(ws + L.slots_at);
     a.n_blocks = n_blocks;
     a.list_parts = parts;
