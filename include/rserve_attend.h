@@ -84,7 +84,8 @@ rs_status rs_kv_append(rs_ctx* ctx, const rs_rotary* rotary, int layer, rs_kv* c
  * Row t of request i is the query at cache slot rs_kv_len - lens[i] + t (its key and value are cached already) and attends to
  * the slots up to its own:  out = sum_k softmax_k(scale q . key_k) value_k,  per head, query head h on KV head h / (Hq / Hkv).
  * lens[i] <= rs_kv_len (RS_EINVAL).  scale: 0 stands for 1 / sqrt(head_dim), else positive and
- * finite, and so, in fp32, is scale log2(e) times an 8-bit cache's keys' scale (RS_EINVAL).  out may be q.
+ * finite, and so, in fp32, is scale log2(e) times an 8-bit cache's keys' scale (RS_EINVAL).  out may be q, with
+ * ld_out = ld_q (RS_EINVAL); rows of out that overlap q in any other way are the caller's error.
  * Scores, softmax statistics and sums are fp32, the softmax's weights enter the second product as bfloat16, the output is
  * rounded once.  What a query does not see does not reach it, infinities and NaN included.
  * Requests of few rows (rows * Hq / Hkv <= 64, or more where little is cached) read 8-bit caches directly, as code * scale; longer ones

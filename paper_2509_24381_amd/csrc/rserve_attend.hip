@@ -352,6 +352,8 @@ rs_status check_attend(const rs_ctx* ctx, int layer, rs_kv* const* kvs, const in
                        float* scale, long* rows) {
     rs_status s = check_call(ctx, layer, kvs, lens, true, R, rows);
     if (s != RS_OK) return s;
+    // (a workgroup's rows of out would be rows of q that another has yet to read)
+    if (*rows > 1 && q && q == out && ld_q != ld_out) return fail(RS_EINVAL, "out is q, but their ld differ: %ld, %ld", ld_q, ld_out);
     for (int i = 0; i < R; ++i)
         if (lens[i] > kvs[i]->len[layer]) return fail(RS_EINVAL, "lens[%d] = %d exceeds the %d cached tokens", i, lens[i], kvs[i]->len[layer]);
     if (*scale == 0.0f) *scale = (float)(1.0 / std::sqrt((double)ctx->cfg.head_dim));
