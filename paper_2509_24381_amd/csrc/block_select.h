@@ -138,6 +138,7 @@ struct SelectArgs {
     int copy_chunks, groups;
 };
 constexpr int SELECT_MAX_BLOCKS = 32768;   // 128 KB of keys
+static_assert(SELECT_MAX_BLOCKS % 4 == 0, "keys of a token are whole 16-byte chunks");
 
 RS_DEVICE uint32_t key_of_score(float s) {
     const uint32_t b = __builtin_bit_cast(uint32_t, s + 0.0f);   // (minus zero is zero)

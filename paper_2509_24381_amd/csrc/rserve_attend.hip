@@ -934,7 +934,7 @@ rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int*
     sa.q = (const bf16*)q; sa.ld_q = ld_q;
     sa.blocks = (int)align_up(longest, 4);
     sa.n_blocks = n_blocks; sa.n_first = n_first; sa.n_last = n_last;
-    sa.tokens = wide ? 1 : (int)std::min<size_t>(4, SELECT_LDS / ((size_t)longest * 4));
+    sa.tokens = wide ? 1 : (int)std::min<size_t>(4, SELECT_LDS / ((size_t)sa.blocks * 4));   // (blocks, at most SELECT_MAX_BLOCKS, which is a multiple of 4 too)
     sa.split = split;
     sa.shared_keys = reinterpret_cast<uint32_t*>(ws + L.keys_at);
     FewArgs a{};
