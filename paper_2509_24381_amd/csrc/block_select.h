@@ -82,7 +82,16 @@ __global__ __launch_bounds__(256) void key_bounds_kernel(int n_req, int hkv, int
 #pragma unroll
     for (int e = 0; e < F; ++e) top = fmaxf(top, fmaxf(hi[e], -lo[e]));
     top = of_row<1>(top, larger_of());
-    const int ex = code_exponent(top);
+    const int ex = __builtin_amdgcn_readfirstlane(code_exponent(top));
+    if (ex > 0) {
+        // A quotient by a unit above one may be too small for fp32, and zero; its code is 1 or -1 all the same.  (Without the branch: 9.2 -> 9.5 us.)
+        const float half = __builtin_ldexpf(0.5f, ex);
+#pragma unroll
+        for (int e = 0; e < F; ++e) {
+            hi[e] = hi[e] > 0.0f ? fmaxf(hi[e], half) : hi[e];
+            lo[e] = lo[e] < 0.0f ? fminf(lo[e], -half) : lo[e];
+        }
+    }
     int8_t* const codes = reinterpret_cast<int8_t*>(rq.codes) + ((size_t)h * rq.room + block) * 2 * D;
     if (lane < CH) {
         union { int8_t b[F]; uint32_t w[F / 4]; } ch, cl;
