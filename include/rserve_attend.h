@@ -72,7 +72,9 @@ rs_status rs_rotary_at(const rs_rotary* rotary, int pos, int pair, float* cos_ou
  * lens[i].  first = rs_kv_len, or starts[i] if `starts` is given: at most rs_kv_len, later tokens are dropped first (drafted
  * tokens that were not accepted; a paged cache keeps the pages that the new length needs).
  *   rotary     null: q and k are not turned
- *   positions  host array, a rotary position per row in [0, rotary max_pos) (RS_ECAPACITY otherwise); null: the cache slots
+ *   positions  host array, a rotary position per row in [0, rotary max_pos) (RS_ECAPACITY otherwise); null: the cache slots.
+ *              Behind rs_prefill_*_mrope a token's position is not its slot, and has to be given.  One number a row is a token whose three
+ *              axes agree, as text's do; tokens whose axes differ are appended by rs_prefill_*_mrope alone.
  *   q, q_out   queries before and after the rotation; q_out may be q (with ld_q_out = ld_q); both null: keys and values only
  * 8-bit caches store codes of the bfloat16 rows, as everywhere.  What the cache holds is the same bits as if the tokens came
  * one by one.  RS_ECAPACITY as in rs_prefill_batch. */

@@ -220,6 +220,18 @@ def _positions_arg(positions):
     return (C.c_int * max(len(flat), 1))(*flat)
 
 
+def _note_positions(kvs, lens, positions, layer: int, axes: int = 3):
+    """Marks the caches whose newest tokens, lens[i] each, were turned by positions (a C array, `axes` per row) other than their slots."""
+    import numpy as np
+    at, row = None, 0
+    for kv, n in zip(kvs, lens):
+        if n > 0 and not kv.own_positions:
+            at = np.ctypeslib.as_array(positions) if at is None else at
+            held = kv.length(layer)
+            kv.own_positions = bool((at[axes * row: axes * (row + n)].reshape(n, axes) != np.arange(held - n, held)[:, None]).any())
+        row += n
+
+
 @dataclass
 class LayerConfig:
     hidden: int
@@ -410,6 +422,9 @@ class KVCache:
         self.handle = C.c_void_p(handle)
         self.slab = slab
         self.pool = pool          # keeps the pool alive as long as the cache
+        # Tokens may have been turned by other rotary positions than their slots (three-axis prompts, kv_append with positions, imports into
+        # a context with sections): who appends behind them has to say where they are.
+        self.own_positions = False
 
     def __del__(self):
         try:
@@ -428,6 +443,7 @@ class KVCache:
 
     def reset(self):
         _check(load_library().rs_kv_reset(self.handle))
+        self.own_positions = False
 
     def truncate(self, layer: int, n_tokens: int):
         _check(load_library().rs_kv_truncate(self.handle, layer, n_tokens))
@@ -449,6 +465,7 @@ class KVCache:
         assert k.is_contiguous() and v.is_contiguous() and k.shape == v.shape
         _check(load_library().rs_kv_import(self.handle, layer, _ptr(k) if n else None, _ptr(v) if n else None, n,
                                            _stream_handle(stream)))
+        self.own_positions |= n > 0 and self.ctx.has_sections
 
     def attach_bounds(self, codes, units):
         """Memory for the bounds on this cache's keys (rs_kv_attach_bounds): codes int8 [n_layers, Hkv, blocks, 2, d], units fp32
@@ -506,12 +523,14 @@ class KVCache:
         assert k.is_contiguous() and v.is_contiguous() and k.shape == v.shape
         _check(load_library().rs_kv_import_codes(self.handle, layer, _ptr(k) if n else None, _ptr(v) if n else None, n,
                                                  _stream_handle(stream)))
+        self.own_positions |= n > 0 and self.ctx.has_sections
 
 
 class Context:
     def __init__(self, cfg: LayerConfig):
         self.cfg = cfg
         self._q_width, self._kv_width = cfg.n_q_heads * cfg.head_dim, cfg.n_kv_heads * cfg.head_dim
+        self.has_sections = False    # three-axis rotary positions (set_mrope_sections)
         self.lib = load_library()
         h = C.c_void_p()
         c = cfg._c()
@@ -614,6 +633,7 @@ class Context:
 
     def set_mrope_sections(self, temporal: int, height: int, width: int):
         _check(self.lib.rs_ctx_set_mrope_sections(self.handle, temporal, height, width))
+        self.has_sections = height > 0 or width > 0
 
     def prefill_batch_mrope(self, packed: PackedWeights, layer: int, kvs: Sequence[KVCache], chunk_lens: Sequence[int],
                             positions, x, y, workspace, stream=None):
@@ -625,6 +645,7 @@ class Context:
         arr_len = (C.c_int * max(r, 1))(*[int(n) for n in chunk_lens])
         _check(self.lib.rs_prefill_batch_mrope(self.handle, C.byref(packed.struct), layer, arr_kv, arr_len, r, arr_pos, _ptr(x),
                                                _ptr(y), _ptr(workspace), workspace.numel(), _stream_handle(stream)))
+        _note_positions(kvs, arr_len, arr_pos, layer)
         return y
 
     def prefill_model_batch(self, layers: Sequence[PackedWeights], kvs: Sequence[KVCache], chunk_lens: Sequence[int],
@@ -648,6 +669,7 @@ class Context:
         arr_len = (C.c_int * max(r, 1))(*[int(n) for n in chunk_lens])
         _check(self.lib.rs_prefill_model_batch_mrope(self.handle, arr_w, len(layers), arr_kv, arr_len, r, arr_pos, _ptr(x), _ptr(y),
                                                      _ptr(workspace), workspace.numel(), _stream_handle(stream)))
+        _note_positions(kvs, arr_len, arr_pos, 0)
         return y
 
     def lm_head(self, final_norm_gain, w_lm, x_rows, stream=None):
@@ -679,6 +701,8 @@ class Context:
         op, ldo = _rows(q_out, "q_out", rows, self._q_width) if q_out is not None else (None, 0)
         _check(self.lib.rs_kv_append(self.handle, rotary.handle if rotary is not None else None, layer, cs.handles, st, n, r, ps, qp, ldq, kp, ldk, vp, ldv, op,
                                      ldo, _stream_handle(stream)))
+        if ps is not None and rotary is not None:
+            _note_positions(cs.caches, n, ps, layer, axes=1)
         return q_out
 
     def attend_workspace(self, max_rows: int, max_requests: int = 1, fp8_visible_tokens: int = 0, n_blocks: int = 0):

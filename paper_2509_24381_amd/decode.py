@@ -11,7 +11,7 @@ from __future__ import annotations
 
 from typing import List, Optional, Sequence
 
-from .binding import CacheSet, Context, KVCache, RotaryConfig, int_array
+from .binding import CacheSet, Context, KVCache, RotaryConfig, RsError, int_array
 from .runner import to_device_bf16
 
 
@@ -32,6 +32,11 @@ class Decoder:
 
     layer_weights: as for runner.LayerStack.  rotary: another rotary form than the context's (None: that one).  n_blocks: blocks of 64
     tokens that a token attends to (0: all); caches of fewer blocks are read whole either way.
+
+    New tokens turn by one rotary position each: their cache slot, or what the caller says.  Behind a prompt with three-axis positions
+    (rs_prefill_*_mrope: an image's tokens share positions) the next token's position is not its slot; the caches know that
+    (KVCache.own_positions), and calls without positions are refused.  A text token there has the same position on all three axes, so that one
+    number says it, and the sections do not matter; tokens whose axes differ go through rs_prefill_*_mrope.
     """
 
     def __init__(self, ctx: Context, layer_weights: Sequence, *, max_rows: int, max_requests: int, rotary: Optional[RotaryConfig] = None,
@@ -42,19 +47,28 @@ class Decoder:
         self.blocks = (n_blocks, n_first, n_last)
         self.ws = ctx.attend_workspace(max_rows, max_requests, fp8_visible_tokens, n_blocks)
 
-    def step(self, kvs, lens, x):
-        """The next lens[i] tokens of every request through all layers: x, and the result, bf16 [sum of lens, H]."""
+    def step(self, kvs, lens, x, positions=None):
+        """The next lens[i] tokens of every request through all layers: x, and the result, bf16 [sum of lens, H].  positions: every row's
+        rotary position, on the host (None: its slot)."""
         import torch
         import torch.nn.functional as F
         ctx, cfg = self.ctx, self.ctx.cfg
         kvs = kvs if isinstance(kvs, CacheSet) else CacheSet(kvs)
         n, (n_blocks, n_first, n_last) = int_array(lens), self.blocks
+        if positions is None:
+            for i, (kv, new) in enumerate(zip(kvs.caches, n)):
+                if new and kv.own_positions:
+                    raise RsError(-1, f"kvs[{i}] holds tokens whose rotary positions are not their slots, or that were imported beside three-axis "
+                                      "sections: give the new tokens' positions")
+        else:
+            positions = int_array(positions.tolist() if hasattr(positions, "tolist") else positions)
         q_dim, kv_dim = cfg.n_q_heads * cfg.head_dim, cfg.n_kv_heads * cfg.head_dim
         q = torch.empty((x.shape[0], q_dim), dtype=torch.bfloat16, device=x.device)
         att = torch.empty_like(q)
         for layer, w in enumerate(self.layers):
             qkv = F.linear(F.rms_norm(x, (cfg.hidden,), w.g1, cfg.rms_eps), w.w_qkv, w.b_qkv)
-            ctx.kv_append(layer, kvs, n, qkv[:, :q_dim], qkv[:, q_dim:q_dim + kv_dim], qkv[:, q_dim + kv_dim:], q, self.rotary)
+            ctx.kv_append(layer, kvs, n, qkv[:, :q_dim], qkv[:, q_dim:q_dim + kv_dim], qkv[:, q_dim + kv_dim:], q, self.rotary,
+                          positions=positions)
             if n_blocks:
                 ctx.attend_blocks(layer, kvs, n, q, att, self.ws, n_blocks, n_first, n_last)
             else:
@@ -75,22 +89,25 @@ class Decoder:
         for kv in kvs:
             kv.new_bounds(capacity_tokens)
 
-    def greedy(self, kvs, last_rows, embedding, final_gain, w_lm, n_tokens: int):
+    def greedy(self, kvs, last_rows, embedding, final_gain, w_lm, n_tokens: int, positions=None):
         """n_tokens tokens of every request, each the likeliest: last_rows is the last layer's output of the prompts' last tokens.
-        embedding [V, H] and w_lm [V, H] bf16.  Returns int64 [requests, n_tokens]."""
+        embedding [V, H] and w_lm [V, H] bf16.  positions: the rotary position of every request's first new token, the others follow it (None: the
+        slots).  Returns int64 [requests, n_tokens]."""
         import torch
         kvs = kvs if isinstance(kvs, CacheSet) else CacheSet(kvs)
         one, out = int_array([1] * len(kvs)), []
-        for _ in range(n_tokens):
+        for t in range(n_tokens):
             out.append(self.ctx.lm_head(final_gain, w_lm, last_rows).argmax(dim=1))
-            last_rows = self.step(kvs, one, embedding[out[-1]])
+            last_rows = self.step(kvs, one, embedding[out[-1]], None if positions is None else [int(p) + t for p in positions])
         return torch.stack(out, dim=1)
 
-    def greedy_drafted(self, kv: KVCache, last_row, embedding, final_gain, w_lm, n_tokens: int, draft):
+    def greedy_drafted(self, kv: KVCache, last_row, embedding, final_gain, w_lm, n_tokens: int, draft, position=None):
         """One request's n_tokens likeliest tokens, several a step: draft(tokens) guesses what follows them, the step checks the guesses
-        together, and those after the first wrong one are dropped from the cache.  Returns (tokens, steps)."""
+        together, and those after the first wrong one are dropped from the cache.  position: the first new token's rotary position, the others
+        follow it (None: the slots).  Returns (tokens, steps)."""
         import torch
         kvs, tokens, steps = CacheSet([kv]), [], 0
+        ahead = None if position is None else int(position) - kv.length(0)   # of the slots
         token = int(self.ctx.lm_head(final_gain, w_lm, last_row).argmax())
         while True:
             tokens.append(token)
@@ -98,7 +115,8 @@ class Decoder:
                 return tokens[:n_tokens], steps
             guesses: List[int] = [int(t) for t in draft(tokens)]
             held = kv.length(0)
-            rows = self.step(kvs, [1 + len(guesses)], embedding[torch.tensor([token] + guesses, device=embedding.device)])
+            at = None if ahead is None else range(held + ahead, held + ahead + 1 + len(guesses))
+            rows = self.step(kvs, [1 + len(guesses)], embedding[torch.tensor([token] + guesses, device=embedding.device)], at)
             best = self.ctx.lm_head(final_gain, w_lm, rows).argmax(dim=1).tolist()
             steps += 1
             taken = 0
