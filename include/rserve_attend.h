@@ -90,8 +90,9 @@ rs_status rs_kv_append(rs_ctx* ctx, const rs_rotary* rotary, int layer, rs_kv* c
  * ld_out = ld_q (RS_EINVAL); rows of out that overlap q in any other way are the caller's error.
  * Scores, softmax statistics and sums are fp32, the softmax's weights enter the second product as bfloat16, the output is
  * rounded once.  What a query does not see does not reach it, infinities and NaN included.
- * Requests of few rows (rows * Hq / Hkv <= 64, or more where little is cached) read 8-bit caches directly, as code * scale; longer ones
- * expand what they see into the workspace first, as rs_prefill_* do (the value is then rounded to bfloat16).
+ * Requests of few rows (rows * Hq / Hkv <= 64, or more where little is cached) read 8-bit caches directly; longer ones expand the codes
+ * that they see to bfloat16 in the workspace first.  A code is exact there, and the scales enter the softmax's scale and the output, so
+ * that either way a key or value is code * scale (rs_prefill_* round that to bfloat16).
  * RS_ATTEND_FEW=n, a TEST-ONLY environment variable read in rs_ctx_create, replaces the size up to which "more rows" are few (0: never).
  *   workspace   256-byte aligned, rs_attend_workspace_bytes:
  *     max_rows, max_requests   of a call

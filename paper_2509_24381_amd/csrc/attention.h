@@ -36,7 +36,7 @@ struct ReqDesc {
     bf16* vtcache;  // contiguous: this layer's V^T [Hkv][cap/64][d][64];  paged: unused
     const int* pages;  // paged: pages[b] = pool page that holds this layer's 64-token block b;  contiguous: null
     int hkv;           // KV heads (a page is [Hkv] K tiles followed by [Hkv] V^T tiles)
-    int pad_;
+    float k_scale, v_scale;   // row-major output only: the tiles hold keys / k_scale and values / v_scale (8-bit caches: their codes)
 };
 
 // Where the 64-token tiles of one KV head live.  A tile is K rows [64][d] or V^T [d][64], either one contiguous run of
@@ -147,7 +147,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_pipelined_kernel(c
                                                                                 const AttnItem* __restrict__ items,
                                                                                 const bf16* __restrict__ qkv, int ld_qkv,
                                                                                 bf16* __restrict__ out, int ld_out,
-                                                                                int g, float scale_log2e,
+                                                                                int g, float call_scale_log2e,
                                                                                 float* __restrict__ split_buf) {
     constexpr int BLOCK_ROWS = 32 * WAVES, THREADS = 64 * WAVES;
     constexpr int KSTEPS = D / 16;
@@ -172,6 +172,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_pipelined_kernel(c
 
     const AttnItem item = items[blockIdx.x];
     const ReqDesc rq = reqs[item.req];
+    const float scale_log2e = ROWS ? call_scale_log2e * rq.k_scale : call_scale_log2e;
     const int rows_total = rq.T * g;
     const int wrow0 = item.qblock * BLOCK_ROWS + wave * 32;
     const int row = wrow0 + l32;
@@ -473,7 +474,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_pipelined_kernel(c
                 } else {
                     bf16* const op = out + (size_t)(rq.row0 + atok) * ld_out + ahead * D;
 #pragma unroll
-                    for (int j = 0; j < D / 64; ++j) op[lane + 64 * j] = f32_to_bf16(eo[j] / el);
+                    for (int j = 0; j < D / 64; ++j) op[lane + 64 * j] = f32_to_bf16(eo[j] / el * rq.v_scale);
                 }
             }
             if ((again >> l32) & 1u) return;   // (this lane's row is done)
@@ -499,7 +500,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_prefill_pipelined_kernel(c
         return;
     }
     if (row < rows_total) {
-        const float inv = 1.0f / l_tot;
+        const float inv = (ROWS ? rq.v_scale : 1.0f) / l_tot;
         if constexpr (ROWS) {
             bf16* const op = out + (size_t)(rq.row0 + tok) * ld_out + head * D + half * 4;
 #pragma unroll
@@ -542,10 +543,11 @@ constexpr int ATT_MERGE_EARLY_WAVES = 12;   // wavefronts per compute unit that 
 template <int D, int WAVES, int MAXP, bool EARLY, bool ROW_MAJOR = false>
 __global__ __launch_bounds__(32 * WAVES) void attn_merge_kernel(const ReqDesc* __restrict__ reqs, const AttnMergeItem* __restrict__ items,
                                                          const float* __restrict__ split_buf, bf16* __restrict__ out, int ld_out,
-                                                         int g, float scale_log2e) {
+                                                         int g, float call_scale_log2e) {
     constexpr int ROWS = 32 * WAVES;
     const AttnMergeItem item = items[blockIdx.x];
     const ReqDesc rq = reqs[item.req];
+    const float scale_log2e = ROW_MAJOR ? call_scale_log2e * rq.k_scale : call_scale_log2e;
     const int rs = threadIdx.x;
     const int row = item.qblock * ROWS + rs;
     if (row >= rq.T * g) return;
@@ -583,7 +585,7 @@ __global__ __launch_bounds__(32 * WAVES) void attn_merge_kernel(const ReqDesc* _
             l_all += w[p] * lp[p];
         }
     }
-    const float inv = 1.0f / l_all;
+    const float inv = (ROW_MAJOR ? rq.v_scale : 1.0f) / l_all;
     const uint32_t m = (uint32_t)(rq.row0 + tok);
     char* const op = reinterpret_cast<char*>(out) + (size_t)(m >> 5) * (size_t)(ld_out >> 4) * 1024 + (m & 31u) * 16u;
     const int ks0 = (head * D) >> 4;

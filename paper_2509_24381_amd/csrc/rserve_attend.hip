@@ -728,6 +728,7 @@ rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, 
             const int len = kv->len[layer];
             ReqDesc d = kv->view(layer, d_pagetab + pagetab.size());
             d.row0 = row; d.T = lens[i]; d.P = len - lens[i];
+            d.k_scale = kv->k_scale; d.v_scale = kv->v_scale;   // (bfloat16 caches: one)
             if (fp8) {
                 Fp8CacheDesc fc{};
                 if (kv->paged()) {
@@ -738,7 +739,7 @@ rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, 
                     fc.kc = kv->kc_of(layer); fc.vc = kv->vc_of(layer); fc.cap = kv->cap;
                 }
                 fc.xb0 = n_xblocks; fc.hkv = f.n_kv_heads;
-                fc.k_scale = kv->k_scale; fc.v_scale = kv->v_scale;
+                fc.k_scale = fc.v_scale = 1.0f;   // (a code is a bfloat16 number, code times scale is not)
                 fp8s.push_back(fc);
                 const size_t plane = expansion_bytes(ctx, len) / 2;
                 d.kcache = reinterpret_cast<bf16*>(ws + expand_at);
