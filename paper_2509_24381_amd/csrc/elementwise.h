@@ -3,6 +3,7 @@
 #pragma once
 #include "attention.h"
 #include "common.h"
+#include "kv_blocks.h"
 
 // ---------------------------------------------------------------- layer input: RMSNorm row factor + fragment-major copy
 // One pass over x: inv_rms[row] = rsqrt(mean(x[row]^2) + eps) (fp32 sums; the factor is applied inside the next GEMM's
@@ -160,7 +161,7 @@ __global__ __launch_bounds__(256) void rms_and_fragment_major_kernel(const bf16*
 
 // ---------------------------------------------------------------- first-token head: final RMSNorm + vocabulary projection
 // h[r][k] = x[r][k] * g[k] * rsqrt(mean(x[r]^2) + eps), kept in fp32.  One wavefront per row.
-static __global__ __launch_bounds__(256) void final_norm_kernel(const bf16* __restrict__ x, const bf16* __restrict__ gain,
+__global__ __launch_bounds__(256) void final_norm_kernel(const bf16* __restrict__ x, const bf16* __restrict__ gain,
                                                          float* __restrict__ h, int rows, int H, float eps) {
     const int lane = threadIdx.x & 63;
     const int row = blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -264,7 +265,7 @@ constexpr int LM_MFMA_ROWS = 3;   // from this many rows on
 constexpr int LM_GROUP = 10;      // rows per B operand
 constexpr int LM_MAX_GROUPS = 2;  // B operands per launch (three spill: 525 us for 30 rows, two passes take 470)
 constexpr int LM_VROWS = 64;      // vocabulary rows per workgroup
-static __global__ __launch_bounds__(256) void final_norm_split_kernel(const bf16* __restrict__ x, const bf16* __restrict__ gain,
+__global__ __launch_bounds__(256) void final_norm_split_kernel(const bf16* __restrict__ x, const bf16* __restrict__ gain,
                                                                bf16* __restrict__ hb, int rows, int H, float eps) {
     // one workgroup per place of a group of rows (grid x: LM_GROUP, + 1 for the two columns that hold no row; grid y: groups)
     const int rg = blockIdx.x;
@@ -470,11 +471,6 @@ __global__ __launch_bounds__(256, 1) void lm_head_mfma_kernel(const bf16* __rest
 }
 
 // ---------------------------------------------------------------- K / V append
-struct KVBlockItem {
-    int req;
-    int block;  // absolute 64-token block index in the request's cache
-};
-
 // One workgroup per (touched 64-token block, KV head).  The rotated k rows are copied from the qkv buffer to the
 // request's K cache (256-byte rows, 16-byte vector copies).  The v rows are transposed through LDS and written as
 // [d][64] with the token index innermost, 16 bytes (8 tokens) per store.  Tokens before P keep their content; V
@@ -542,7 +538,7 @@ __global__ __launch_bounds__(256) void append_kv_kernel(const bf16* __restrict__
 // `wide`: the source can be read 16 bytes at a time.
 constexpr int PACK_K = 256;
 enum PackMode { PACK_IDENTITY = 0, PACK_GATE_UP = 1, PACK_QKV_ROPE = 2 };
-static __global__ __launch_bounds__(256) void pack_rows_kernel(const bf16* __restrict__ src, const bf16* __restrict__ gain,
+__global__ __launch_bounds__(256) void pack_rows_kernel(const bf16* __restrict__ src, const bf16* __restrict__ gain,
                                                         bf16* __restrict__ dst, int K, int mode, int p0, int p1, int wide) {
     constexpr int CH = PACK_K / 8;   // 16-byte chunks of a row
     __shared__ uint4 tile[32][CH + 1];   // (rows one chunk further: 16 rows' reads of one chunk cover all banks)
@@ -589,21 +585,4 @@ static __global__ __launch_bounds__(256) void pack_rows_kernel(const bf16* __res
         const int co = (int)(threadIdx.x >> 5) + i * 8;
         if (c0 + co < K / 8) st_global_16_stream(d + (size_t)(c0 + co) * 256, tile[t][co]);
     }
-}
-
-// ---------------------------------------------------------------- tiles of a cache in export / import (kv_transfer.h)
-// The cache is described like a request (ReqDesc: contiguous planes, or the pool base for a paged cache).  The page
-// numbers of a paged cache travel in the kernel arguments, a window of KV_PAGE_WINDOW blocks per launch starting at
-// block `block0`; tokens [t0, t0 + n) are handled, t0 a multiple of 64 inside the window.
-constexpr int KV_PAGE_WINDOW = 256;
-struct KVPageWindow {
-    int page[KV_PAGE_WINDOW];
-};
-
-template <int D>
-RS_DEVICE bf16* kv_window_tile(const ReqDesc& rq, const KVPageWindow& win, int block0, bool v, int c, int block) {
-    constexpr size_t TILE = (size_t)64 * D;  // elements
-    if (rq.pages == nullptr)   // (any non-null value marks a paged cache here; the numbers come from the window)
-        return (v ? rq.vtcache : rq.kcache) + ((size_t)c * (size_t)(rq.cap >> 6) + (size_t)block) * TILE;
-    return rq.kcache + ((size_t)win.page[block - block0] * 2 * rq.hkv + (size_t)(v ? rq.hkv : 0) + (size_t)c) * TILE;
 }

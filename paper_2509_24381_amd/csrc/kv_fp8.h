@@ -12,7 +12,7 @@
 #pragma once
 #include "attention.h"
 #include "common.h"
-#include "elementwise.h"
+#include "kv_blocks.h"
 
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 

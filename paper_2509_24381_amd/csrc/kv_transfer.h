@@ -17,7 +17,7 @@
 #pragma once
 #include "attention.h"
 #include "common.h"
-#include "elementwise.h"
+#include "kv_blocks.h"
 #include "kv_fp8.h"
 
 // 8 stored elements <-> 8 canonical ones
