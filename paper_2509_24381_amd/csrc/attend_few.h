@@ -8,7 +8,7 @@
 // streams its own through its own LDS, by DMA, without barriers, in units of 4 KB - a quarter of a tile's keys, then of its values - and two
 // places: the unit after the next is under way as soon as this one is in registers.  (Loads straight into the MFMA operand layout, where
 // neighbouring lanes are different keys, need no LDS, but the address unit then takes 64 clocks for a load of a KB instead of 16: a
-// compute unit gets 16 bytes per clock, whatever the cache they come from.)  A workgroup takes 34 KB of LDS and 114 registers, so that four share
+// compute unit gets 16 bytes per clock, whatever the cache they come from.)  A workgroup takes 34 KB of LDS and 115 to 120 registers (d = 128), so that four share
 // a compute unit; units of 8 KB and two of them: one token on 2000 11.7 us a pass instead of 10.3, selected blocks 59.6 instead of 57.3.
 //
 // As in the chunk kernel (attention.h) the transposed products keep a query in one lane (lane & 15):
@@ -20,13 +20,14 @@
 // difference times the scale: zero, exactly, for the key that is the reference.  (With the scale in the reference, whose rounding an fma does not
 // repeat, all weights of a row move by that rounding, and from scores of 2^32 on out of fp32's range.)
 //  A weight becomes bfloat16 for the second product, whose operands have 16 bits; the row
-// sum takes it before that.  The output is rounded once.  A masked key has weight zero; where its value is an infinity or NaN the row
+// sum takes it before that.  The output is rounded once.  (Errors against 64 bits are 0.0021 to 0.0023 of the output then; 0.0017, the output's own
+// rounding, with weights of 32 bits, which would take a second product for what the first leaves of each.)  A masked key has weight zero; where its value is an infinity or NaN the row
 // comes out not finite and is done again by exact_row, which leaves masked values alone.
 //
 // Work item = (request, KV head, part of the key range), with up to 64 stacked rows.  A wavefront has 16 of them (RB = 1), and with up to 16
 // rows the four wavefronts of a workgroup share the item's tiles, with up to 32 two pairs do, with more each takes every tile, which the
-// others' loads have brought into the caches; or it has 32 (RB = 2), so that tiles are loaded half as often, for 179 registers instead of
-// 120 and longer chains.  They meet in LDS once per 16 rows; parts leave unnormalised sums, references and row sums in slots that
+// others' loads have brought into the caches; or it has 32 (RB = 2), so that tiles are loaded half as often, for 174 to 179 registers
+// and longer chains.  They meet in LDS once per 16 rows; parts leave unnormalised sums, references and row sums in slots that
 // few_merge_kernel joins.
 //
 // Measured, us of this kernel (28 query heads, 4 KV heads, d = 128): one token on 2000, 4.1 MB, 6.3 and the merge 3.8, what dependent loads
@@ -548,9 +549,10 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void attend_few_kernel(FewArgs a
     attend_rows<D, FP8, LIST, RB>(a, rq, pages, rows, part, parts, unit, n, list, lds, m_sh, l_sh);
 }
 
-// Joins the parts of 16 rows:  M = max_p m_p,  out = sum_p 2^(c (m_p - M)) O_p / sum_p 2^(c (m_p - M)) l_p, c the scale.  One workgroup per 16 rows and 32
+// Joins the parts of 16 rows:  M = max_p m_p,  out = sum_p 2^(c (m_p - M)) O_p / sum_p 2^(c (m_p - M)) l_p, c the scale log2e.  One workgroup per 16 rows and 32
 // features, a quarter of the parts per 64 threads (16 rows x 4 chunks of 8 features).  3 to 5 us, the latency of a launch and of loads that
-// follow one another.  (Joining in the kernel before, by the last workgroup to arrive, needs a fence across the chip: 64 single tokens 84 -> 198 us.)
+// follow one another.  (Joining in the kernel before, by the last workgroup to arrive, behind a fence across the chip: 64 single tokens 84 -> 198 us; with slots that are
+// themselves stored and loaded past the L2s, without a fence, it has not been measured.)
 template <int D, bool LIST, class Tab>
 __global__ __launch_bounds__(256) void few_merge_kernel(FewArgs a, Tab tab) {
     __shared__ float m_sh[4][16];

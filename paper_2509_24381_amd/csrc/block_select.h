@@ -120,8 +120,8 @@ __global__ __launch_bounds__(256) void key_bounds_kernel(int n_req, int hkv, int
 // These are the kernels for many tokens, many requests and very long caches; otherwise attend_selected_kernel takes the same steps itself.
 // With many tokens a workgroup has four, a wavefront each, and takes all three steps.  With few (WIDE) it has one, and where that has more
 // blocks than a workgroup scores at once, the first two steps are a launch of their own, of a workgroup per 256 blocks: a compute unit alone
-// gets 33 bytes per ns, 16 us for the bounds of 2046 blocks.  (One launch, the last workgroup to finish selecting: the fence that makes
-// keys visible across the chip takes longer than a second launch, 7 us.)
+// gets 33 bytes per ns, 16 us for the bounds of 2046 blocks.  (One launch, the last workgroup to finish selecting, behind the fence that makes
+// keys visible across the chip: longer than a second launch, 7 us.  Keys stored and loaded past the L2s, without a fence, have not been measured.)
 // Measured: one token on 2046 blocks 6.0 and 6.2 us, 256 tokens on 250 blocks 10.6: chains from queries to codes, scores, digits, list.  (Reductions
 // over lanes stay in registers; through LDS the three took 7.3, 7.5 and 12.4.)
 struct SelectReq {          // 64 bytes

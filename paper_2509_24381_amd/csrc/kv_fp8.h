@@ -2,13 +2,15 @@
 //
 //   stored  code  = e4m3( fl32( x * fl32(1 / scale) ) )      x: the bfloat16 K~ or V element; nearest, ties to even,
 //                                                             saturating at +-448, NaN -> 0x7f
-//   read    value = bf16( fl32( decode(code) * scale ) )
+//   read    value = bf16( fl32( decode(code) * scale ) ) by rs_prefill_*, export;  decode(code) * scale by rs_attend, rs_attend_blocks
 //
 // The cache keeps the tile layout of the bfloat16 one with one byte per element: per KV head, K tiles [64 tokens][d]
-// and V^T tiles [d][64 tokens], contiguous per layer or in pages of 64 tokens.  The attention kernels do not read it: before attention, the blocks a call's rows can see
-// are expanded to bfloat16 tiles in the call's workspace (one layer's worth, reused by every layer), which the unchanged
-// attention kernel then walks.  Expanding costs one pass over the prefix at HBM speed (a few microseconds per 10k
-// tokens), far less than converting inside the attention loop, whose limit is LDS bandwidth and issue slots, not HBM.
+// and V^T tiles [d][64 tokens], contiguous per layer or in pages of 64 tokens.  The chunk kernel (attention.h) does not read it: the blocks a call's rows can see
+// are expanded to bfloat16 tiles in the call's workspace first (one layer's worth, reused by every layer), which the unchanged
+// kernel then walks.  Expanding costs one pass over the prefix at HBM speed (a few microseconds per 10k
+// tokens; a chunk of 256 rows on 30000, with the expansion 131 us a pass, on a bfloat16 cache 118), less than converting inside its loop, whose limit is LDS
+// bandwidth and issue slots, not HBM.  The kernels for few rows and for selected blocks (attend_few.h, attend_selected.h), which are bound by HBM,
+// load the codes and convert them in registers.
 #pragma once
 #include "attention.h"
 #include "common.h"

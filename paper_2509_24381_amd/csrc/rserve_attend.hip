@@ -39,6 +39,9 @@ namespace {
 // (3756) 65.1 / 52.3; (h) 48 on 4000 (3024) 79.1 / 73.4; beside 30 on 300: (g) 96 on 4000 (2772) 37.5 / 28.8, (h) 64 on 2000 (2048) 38.4 / 28.0,
 // 96 on 4000 (6048) 46.2 / 54.8; beside 60 on 4000, (g) 128 on 4000 (3528) 109.8 / 100.0, (h) (8064) 184 / 215.  8 bits: (h) 12 on 16000 (4000)
 // 46.9 / 24.6, 100 on 4000 (6552) 41.4 / 37.2; beside 30 on 300, 96 on 4000 (6048) 47.9 / 50.5; beside 60 on 4000, 128 on 4000 (8064) 122.4 / 143.5.
+// One product does not tell few rows on long caches from many on short ones, and near its bounds the rule takes the slower side: of the lines above
+// 12 on 20000, 8 bits 100 on 4000 and beside 30 on 300, 96 on 4000; farther out, (g) 12 on 64000 68.6 / 43.9, 16 on 20000 32.6 / 26.0, on 64000
+// 69.6 / 43.3, 32 on 64000 72.5 / 66.8, where (h) has the chunk kernel ahead: 12 on 64000 73.1 / 74.5, 32 on 20000 41.5 / 49.7, on 64000 99.2 / 127.0.
 constexpr int FEW_ROWS = FEW_GROUP;
 constexpr long FEW_TILES = 2500, FEW_TILES_BESIDE = 5000, FEW_TILES_FP8 = 6500;
 // Where a request has more than 32 rows in a group, wavefronts get 32 rows instead of 16 if the call has this many tiles (times KV heads and
