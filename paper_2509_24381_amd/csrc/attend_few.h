@@ -39,6 +39,7 @@
 #include "call_tables.h"
 #include "common.h"
 #include "exact_row.h"
+#include "few_plan.h"
 #include "lanes.h"
 #include "kv_fp8.h"
 
@@ -73,7 +74,6 @@ struct FewShared {
 };
 constexpr int SHARED_WORDS = 6;
 static_assert(sizeof(FewShared) == 4 * SHARED_WORDS, "SHARED_WORDS");
-constexpr int NOBODY = 0xffff, SEVERAL = 0xfffe;
 
 // Eight E4M3 codes to bfloat16, exactly.
 RS_DEVICE bf16x8 bf16x8_of_codes(uint32_t lo, uint32_t hi) {
@@ -115,19 +115,13 @@ RS_DEVICE const FewShared* shared_requests(const uint32_t* table, int n_req) { r
 RS_DEVICE const uint32_t* shared_pages(const FewArgs& a, const uint32_t* table) { return a.pages ? a.pages : table + table_reqs_at(a.n_req) + SHARED_WORDS * a.n_req; }
 
 #define RS_UNIT __device__ __forceinline__
-constexpr int FEW_WAVES = 4;
-constexpr int FEW_MAX_PARTS = 64;
 constexpr float FEW_HEADROOM = 8.0f;   // the reference moves when a score exceeds it by this many powers of two
-
-// Blocks of 16 rows that `rows` of them are handled as: 1, 2 or 4.
-__host__ __device__ inline int few_row_blocks(int rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
 
 template <int D>
 struct FewSlot {   // of a part and 16 rows: [16][D] sums, then references, then row sums
     static constexpr size_t FLOATS = (size_t)16 * (D + 2);
 };
 
-constexpr int FEW_GROUP = 64;          // stacked rows of an item
 // An item's rows, and where they are in q and out.
 template <bool LIST>
 struct FewRows {

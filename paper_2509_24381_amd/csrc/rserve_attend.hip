@@ -16,6 +16,7 @@
 #include "attention.h"
 #include "block_select.h"
 #include "cache_calls.h"
+#include "few_plan.h"
 #include "host_state.h"
 #include "kv_fp8.h"
 #include "last_error.h"
@@ -62,10 +63,6 @@ constexpr int FEW_PLACES = 2;
 // (246) 25.3 / 19.5, 16 x 4 on 8000 (444) 72.7 / 43.5; (h) 4 x 4 on 2000 (59) 17.1 / 15.5, 1 x 8 on 4000 (114) 18.3 / 17.7, 4 x 16 on 8000 (1190) 105 / 46;
 // 8 bits: (g) 4 x 4 on 4000 (29) 14.7 / 15.3, 1 x 8 on 8000 (57) 16.5 / 18.8, 16 x 4 on 8000 (222) 43.7 / 32.7, (h) 4 x 16 on 32000 (2390) 227 / 76.
 constexpr size_t SHARED_BYTES = (size_t)60 << 20;
-// Wavefronts of a workgroup share tiles (attend_shared.h) where a request has more than 32 stacked rows, and where it has more than 16 if the call's requests of
-// that kind have this many tiles, times KV heads.  us a pass, wavefronts apart / together: (g) 4 beams each, 1 on 8000 (500) 15.7 / 16.6, 4 on 2000 (300)
-// 13.0 / 13.8, 1 on 32000 (2000) 22.9 / 25.8, 16 on 8000 (4520) 51.4 / 43.5, 8 bits 34.7 / 32.7; 8 beams, 8 on 8000 (2130) 37.7 / 32.0.
-constexpr long TOGETHER_TILES = 3000;
 constexpr size_t SLOT_ROWS = 65536;   // rows there is room for in the slots of split key ranges
 // Tokens times KV heads up to which a workgroup selects for one token, and several share its blocks; beyond, for four.  us a pass, four / one, 4 KV
 // heads: 16 tokens on 8000 20.2 / 19.3, on 60000 34.7 / 27.3; 64 on 16000 29.2 / 28.7, on 60000 42.1 / 40.4; 96 on 16000 34.8 / 35.5; 128 on 60000 47.6 / 51.7.
@@ -176,57 +173,6 @@ AttendLayout attend_layout(const rs_layer_cfg& f, int max_rows, int max_requests
 size_t expansion_bytes(const rs_ctx* c, long tokens) { return (size_t)2 * align_up((size_t)tokens, 64) * c->kv_dim * 2; }
 
 // ---------------------------------------------------------------- few rows
-// Parts of the key ranges, of `len` tiles at most.  Estimated in tiles of a place (a workgroup's room on a compute unit) when all places stream:
-// an item costs 1.5 beside its tiles, joining 2.  With no more items than places the longest ends last, but the fewer are left the
-// faster they stream: a tile then takes 0.66 of one.  With more, the last ones start late: a share of the longest comes on top.  Where two or
-// all four wavefronts need every tile it takes 2 and 3 times as long (wavefronts of 32 rows: 1.5 and 2), and parts are that much shorter (us a
-// pass, all alike -> so: 30 single tokens on up to 8000 beside 4 requests of 5 on 3000, 64 query heads, 8 KV heads, 142.7 -> 115.5, 8 bits
-// 91.3 -> 55.8; 24 requests of 3 on up to 6000 beside one of 12 on 5000 68.4 -> 53.4; one of 4 on 8000, alone, 15.8 -> 17.2).
-// us a pass, parts of 4 / 8 / 16 / 24 / 48 tiles, and with this estimate's: 64 requests on up to 8000 tokens 97.4 / 93.2 / 86.0 / 86.6 / 89.0,
-// 88.3; 16 on up to 32000, 8 bits, 73.2 / 68.6 / 66.1 / 64.6 / 59.4, 60.2; 24 of 3 tokens on up to 6000 and one of 12, 64 and 8 heads, 79.6 / 69.5 / 58.3 / 56.6 / 67.0, 54.3.
-struct FewRequest {
-    int kv, row0, T;       // index into kvs, first row, rows
-    int units, tiles;      // items per part, tiles
-    int row_blocks;        // of 16 rows: 1, 2 or 4
-    int parts;
-    bool once = false;     // its tiles are read once
-    double weight = 1.0;   // of a tile
-    int tile0 = 0;         // first of its tiles
-    int with = NOBODY;     // (FewShared)
-    int together = 0;      // (FewShared)
-    bool in_slots() const { return parts > 1 || with != NOBODY; }
-    double work() const { return tiles * weight; }
-    int parts_of(int len) const { return std::min((int)std::ceil(work() / len), FEW_MAX_PARTS); }
-};
-void plan_few(std::vector<FewRequest>& reqs, int places, size_t slots) {
-    double total = 0.0;
-    int longest = 1;
-    for (const FewRequest& r : reqs) {
-        total += r.units * r.work();
-        longest = std::max(longest, (int)std::ceil(r.work()));
-    }
-    double best = 1e30;
-    int best_len = longest;
-    for (int len = FEW_WAVES; ; len = std::min(longest, len + std::max(1, len / 8))) {
-        long items = 0, split = 0;
-        double most = 0.0;
-        for (const FewRequest& r : reqs) {
-            const int p = r.parts_of(len);
-            items += (long)r.units * p;
-            if (p > 1 || r.with != NOBODY) split += (long)r.units * p * r.row_blocks;
-            most = std::max(most, (r.tiles + p - 1) / p * r.weight * 0.66);
-        }
-        const double share = total / places;
-        const double cost = (items <= places ? std::max(share, most) + 1.5 : share + 1.5 * items / places + 0.5 * most) + (split ? 2.0 : 0.0);
-        if ((size_t)split <= slots && cost < best) {
-            best = cost;
-            best_len = len;
-        }
-        if (len >= longest) break;
-    }
-    for (FewRequest& r : reqs) r.parts = r.parts_of(best_len);
-}
-
 // The table of `reqs` at `w` (`words` of room, checked by the caller), their page numbers at `pages`.  LIST: items are rows.
 struct FewTable {
     uint32_t items = 0, units = 0;
@@ -320,11 +266,8 @@ bool share_pages(const rs_ctx* ctx, int layer, rs_kv* const* kvs, std::vector<Fe
     }
     if (several.empty()) return false;
     several.insert(several.end(), reqs.begin(), reqs.end());
-    long slots = 0;
-    for (const FewRequest& r : several)
-        if (r.with != NOBODY) slots += (long)r.units * r.row_blocks;
     const size_t tile_bytes = (size_t)128 * ctx->kv_dim * (kvs[reqs[0].kv]->fp8 ? 1 : 2);   // of all KV heads
-    if ((size_t)unread_tiles * tile_bytes < (ctx->shared_bytes >= 0 ? (size_t)ctx->shared_bytes : SHARED_BYTES) || 2 * slots > (long)(SLOT_ROWS / 16)) {   // (or no room for their sums, of halves of tiles perhaps)
+    if ((size_t)unread_tiles * tile_bytes < (ctx->shared_bytes >= 0 ? (size_t)ctx->shared_bytes : SHARED_BYTES) || 2 * fewest_slots(several) > SLOT_ROWS / 16) {   // (or no room for their sums: see share_tiles)
         for (FewRequest& r : reqs) {
             r.tiles += r.tile0;
             r.tile0 = 0;
@@ -727,21 +670,7 @@ rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, 
     size_t few_words = 0, few_pages = 0, few_bytes = 0;   // few_bytes: of the keys and values they read
     if (!few.empty()) {
         shared = few.size() > 1 && share_pages(ctx, layer, kvs, few);
-        long shared_tiles = 0;
-        const long together_from = ctx->together_tiles >= 0 ? ctx->together_tiles : TOGETHER_TILES;
-        for (const FewRequest& r : few)
-            if (r.with == SEVERAL) shared_tiles += (long)r.units * r.tiles;
-        const auto shares_tiles = [&](const FewRequest& r) { return r.with == SEVERAL && r.row_blocks > (shared_tiles >= together_from ? 1 : 2); };
-        for (const FewRequest& r : few)
-            if (shares_tiles(r)) together = std::max(together, (long)r.T * ctx->group > FEW_GROUP ? 2 : 1);
-        if (together)
-            for (FewRequest& r : few) {
-                if (!shares_tiles(r)) continue;
-                r.together = together;
-                const int groups = (int)(((long)r.T * ctx->group + FEW_GROUP * together - 1) / (FEW_GROUP * together));
-                r.units = groups * f.n_kv_heads;
-                r.row_blocks = 2 * FEW_GROUP / 16;   // (slots: of 128 rows, or of 64 twice)
-            }
+        if (shared) together = share_tiles(few, ctx->group, f.n_kv_heads, ctx->together_tiles >= 0 ? ctx->together_tiles : TOGETHER_TILES, SLOT_ROWS / 16);
         for (const FewRequest& r : few) few_bytes += (size_t)r.tiles * 128 * ctx->kv_dim * (fp8 ? 1 : 2);
         long all_tiles = 0;
         for (const FewRequest& r : few) {
@@ -753,7 +682,7 @@ rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, 
             r.once = few_bytes >= FEW_ONCE_BYTES && (r.together ? r.units == f.n_kv_heads : r.row_blocks == 1);
             r.weight = r.together ? 1.0 : pairs ? (r.row_blocks == 1 ? 1.0 : r.row_blocks == 2 ? 1.5 : 2.0) : (r.row_blocks == 1 ? 1.0 : r.row_blocks == 2 ? 2.0 : 3.0);
         }
-        plan_few(few, FEW_PLACES * ctx->n_cu, SLOT_ROWS / 16);
+        if (!plan_few(few, FEW_PLACES * ctx->n_cu, SLOT_ROWS / 16)) return fail(RS_EINVAL, "internal: sums beyond the slots");
         a.n_req = (int)few.size();
         a.hkv = f.n_kv_heads; a.g = ctx->group;
         a.q = (const bf16*)q; a.ld_q = ld_q; a.out = (bf16*)out; a.ld_out = ld_out;
