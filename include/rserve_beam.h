@@ -56,7 +56,8 @@ rs_status rs_beam_select(rs_ctx* ctx, const void* logits, int type, long ld_logi
  * beams' caches go with srcs[i] = caches[parents[i]], dsts = caches.  The caches of a pair have equally many layers and the same kind,
  * 8-bit ones the same scales (RS_EINVAL).  A cache is a destination once (RS_EINVAL).
  * Caches on one pool share its pages, and nothing is launched.  Between all others (contiguous ones, other pools) the tokens are
- * copied: RS_ECAPACITY without room, and a source that has to be copied is no other pair's destination (RS_EINVAL).
+ * copied: RS_ECAPACITY without room, and a source that has to be copied is no other pair's destination (RS_EINVAL).  Where a launch of
+ * these copies fails (RS_EHIP), destinations that are copied into are empty.
  * Bounds (rs_kv_attach_bounds) stay valid for blocks that the destination held already, in the same pages.
  *   rs_kv_shared_pages   pages of `layer` that other caches hold too (-1 on a bad argument; 0 for a contiguous cache) */
 rs_status rs_kv_fork(rs_ctx* ctx, rs_kv* const* srcs, rs_kv* const* dsts, const int* n_tokens, int R, void* hip_stream);

@@ -87,8 +87,9 @@ rs_status launch_moves(rs_ctx* ctx, bool fp8, const std::vector<Move>& moves, co
                 else hipLaunchKernelGGL((kv_copy_kernel<D, FP8, Tab>), dim3(items, 2u * a.hkv * CopyPiece<D, FP8>::PIECES), dim3(256), 0, st, a, table);
             });
         });
-        RS_HIP(hipGetLastError());
-        if (!inside && (s = ring_commit(ctx, st)) != RS_OK) return s;
+        const hipError_t launched = hipGetLastError();
+        if (!inside && (s = ring_commit(ctx, st)) != RS_OK) return s;   // (whatever has failed: page numbers may be read all the same)
+        RS_HIP(launched);
         i0 = i1;
     }
     return RS_OK;
@@ -316,7 +317,15 @@ rs_status rs_kv_fork(rs_ctx* ctx, rs_kv* const* srcs, rs_kv* const* dsts, const 
     std::sort(moves.begin(), moves.end(), [](const Move& x, const Move& y) {   // by source and length (what lands where does not depend on their order)
         return std::make_tuple((uintptr_t)x.from_pages, x.from.k, x.n) < std::make_tuple((uintptr_t)y.from_pages, y.from.k, y.n);
     });
-    return launch_moves(ctx, srcs[0]->fp8, moves, nullptr, st);
+    if ((s = launch_moves(ctx, srcs[0]->fp8, moves, nullptr, st)) == RS_OK) return RS_OK;
+    for (int i = 0; i < R; ++i) {   // nobody knows what has been copied
+        if (shares(i) || srcs[i] == dsts[i]) continue;
+        for (int l = 0; l < dsts[i]->n_layers; ++l) {
+            dsts[i]->len[l] = 0;
+            if (dsts[i]->paged()) dsts[i]->give_back_pages(l, 0);
+        }
+    }
+    return s;
 } catch (const std::exception& e) {
     return not_allocated(e);
 }

@@ -1,0 +1,42 @@
+"""GPU: what calls on caches leave behind when a launch reports an error.  The error is one that a call of somebody else's left, a device that is not
+there; the kernels run."""
+import pytest
+import torch
+
+from tests.test_gpu_cache_operators import context, gen, normal
+
+pytestmark = pytest.mark.gpu
+
+
+def fails(ctx, call):
+    """Runs a call that finds an error behind its first launch."""
+    from paper_2509_24381_amd.binding import RsError
+    assert ctx.lib.hipSetDevice(1 << 20) != 0
+    with pytest.raises(RsError) as e:
+        call()
+    assert e.value.status_name == "RS_EHIP" and "invalid device" in str(e.value)
+    ctx.lib.hipGetLastError()
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("n", [100, 64 * 700])
+@pytest.mark.parametrize("kind", ["contiguous", "paged"])
+def test_a_fork_whose_copies_fail_leaves_empty_caches(kind, n):
+    """Copied destinations; those that share pages are what the call says.  (700 blocks: their numbers are staged.)"""
+    from paper_2509_24381_amd.binding import KVPool
+    ctx, g = context(4, 2, 64, max_pos=64 * 800), gen(1)
+    pool, other = KVPool(ctx, 1500), KVPool(ctx, 1500)
+    src, sharer = pool.new_cache(1), pool.new_cache(1)
+    dst = other.new_cache(1) if kind == "paged" else ctx.kv_alloc(1, 64 * 800)
+    k, v, old = normal(g, n, 2, 64), normal(g, n, 2, 64), normal(g, 300, 2, 64)
+    src.import_(0, k, v)
+    dst.import_(0, old, old)
+    fails(ctx, lambda: ctx.kv_fork([src, src], [dst, sharer]))
+    assert dst.length() == 0 and sharer.length() == src.length() == n
+    if kind == "paged":
+        assert other.free_pages == 1500
+    for _ in range(20):
+        ctx.kv_fork([src], [dst])
+    for kv in (dst, sharer, src):
+        got = kv.export(0)
+        assert torch.equal(got[0], k) and torch.equal(got[1], v)
