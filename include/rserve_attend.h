@@ -77,7 +77,8 @@ rs_status rs_rotary_at(const rs_rotary* rotary, int pos, int pair, float* cos_ou
  *              axes agree, as text's do; tokens whose axes differ are appended by rs_prefill_*_mrope alone.
  *   q, q_out   queries before and after the rotation; q_out may be q (with ld_q_out = ld_q); both null: keys and values only
  * 8-bit caches store codes of the bfloat16 rows, as everywhere.  What the cache holds is the same bits as if the tokens came
- * one by one.  RS_ECAPACITY as in rs_prefill_batch. */
+ * one by one.  RS_ECAPACITY as in rs_prefill_batch.  Where a launch fails (RS_EHIP) the caches end where their new tokens were to begin, or with
+ * the block before, if that one is shared with other caches (rserve_beam.h). */
 rs_status rs_kv_append(rs_ctx* ctx, const rs_rotary* rotary, int layer, rs_kv* const* kvs, const int* starts, const int* lens, int R,
                        const int* positions, const void* q, long ld_q, const void* k, long ld_k, const void* v, long ld_v,
                        void* q_out, long ld_q_out, void* hip_stream);

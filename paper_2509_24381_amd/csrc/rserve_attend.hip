@@ -553,7 +553,19 @@ rs_status rs_kv_append(rs_ctx* ctx, const rs_rotary* rotary, int layer, rs_kv* c
     if (rows == 0) return RS_OK;
     for (int i = 0; i < R && need.copies(); ++i)
         if (copied_from[i] >= 0) kvs[i]->pool->read_slots[copied_from[i]] = 0;
-    if (apart && (s = launch_page_copies(ctx, fp8, copies, st)) != RS_OK) return s;
+    // A launch has failed: nothing is left of the call, nor of the blocks that it went on with in pages of their own.
+    const auto without = [&](rs_status failed) {
+        for (int i = 0; i < R; ++i) {
+            rs_kv* kv = kvs[i];
+            if (lens[i] == 0) continue;
+            const int first = kv->len[layer] - lens[i], left = need.copies() && copied_from[i] >= 0 ? first / 64 * 64 : first;
+            kv->dropped_from(layer, left);
+            kv->len[layer] = left;
+            if (kv->paged()) kv->give_back_pages(layer, left);
+        }
+        return failed;
+    };
+    if (apart && (s = launch_page_copies(ctx, fp8, copies, st)) != RS_OK) return without(s);
     AppendArgs a{};
     a.q = (const bf16*)q; a.k = (const bf16*)k; a.v = (const bf16*)v; a.q_out = (bf16*)q_out;
     a.ld_q = ld_q; a.ld_k = ld_k; a.ld_v = ld_v; a.ld_q_out = ld_q_out;
@@ -604,7 +616,8 @@ rs_status rs_kv_append(rs_ctx* ctx, const rs_rotary* rotary, int layer, rs_kv* c
                 else go(std::false_type{}, std::false_type{});
             });
         });
-        RS_HIP(hipGetLastError());
+        const hipError_t launched = hipGetLastError();
+        if (launched != hipSuccess) return without(fail(RS_EHIP, "append: %s", hipGetErrorString(launched)));
         i0 = i1;
     }
     return RS_OK;

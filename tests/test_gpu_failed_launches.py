@@ -40,3 +40,35 @@ def test_a_fork_whose_copies_fail_leaves_empty_caches(kind, n):
     for kv in (dst, sharer, src):
         got = kv.export(0)
         assert torch.equal(got[0], k) and torch.equal(got[1], v)
+
+
+@pytest.mark.parametrize("apart", [False, True], ids=["in one launch", "copies apart"])
+def test_an_append_that_fails_leaves_what_nobody_had_to_copy(apart):
+    """A cache that continues a shared block in a page of its own ends before that block, others where the call began."""
+    from paper_2509_24381_amd.binding import KVPool
+    ctx, g = context(4, 2, 64), gen(2)
+    pool = KVPool(ctx, 40)
+    pool.slab.fill_(0xFF)   # (NaN)
+    a, alone, flat = pool.new_cache(1), pool.new_cache(1), ctx.kv_alloc(1, 512)
+    k, v = normal(g, 100, 2, 64), normal(g, 100, 2, 64)
+    for kv in (a, alone, flat):
+        kv.import_(0, k, v)
+    b, c = a.fork(), a.fork()
+    kvs = [b, c, a, alone, flat]
+    starts = [100, 100, 70 if apart else 100, 100, 100]   # (what a drops is what the others copy: the last one left does not copy)
+    new, free = normal(g, 5 * 3, 2, 64), pool.free_pages
+    fails(ctx, lambda: ctx.kv_append(0, kvs, [3] * 5, None, new, new, None, starts=starts))
+    assert [kv.length() for kv in kvs] == [64, 64, starts[2], 100, 100]
+    assert pool.free_pages == free   # (the last blocks of b and c are gone, a has its page for itself)
+    for i, kv in enumerate(kvs):
+        n = kv.length()
+        got = kv.export(0)
+        assert torch.equal(got[0], k[:n]) and torch.equal(got[1], v[:n]), i
+    q = normal(g, 5 * 3, 4 * 64)
+    ctx.kv_append(0, kvs, [3] * 5, None, new, new, None)
+    out = ctx.attend(0, kvs, [3] * 5, q, torch.empty_like(q), ctx.attend_workspace(15, 5))
+    fresh = [ctx.kv_alloc(1, 512) for _ in kvs]
+    for kv, other, i in zip(kvs, fresh, range(5)):
+        n = kv.length() - 3
+        other.import_(0, torch.cat((k[:n], new[3 * i: 3 * i + 3])), torch.cat((v[:n], new[3 * i: 3 * i + 3])))
+    assert torch.equal(out, ctx.attend(0, fresh, [3] * 5, q, torch.empty_like(q), ctx.attend_workspace(15, 5)))
