@@ -870,8 +870,9 @@ rs_status prefill_enqueue(rs_ctx* ctx, const rs_layer_weights* w, int layer, rs_
     const int H = f.hidden, I = f.mlp_inter;
     const StepTimer tm{ctx, st};
 
-    rollback.armed = false;   // every host-side check has passed: from here on the call is launched
+    // every host-side check has passed: from here on the call is launched
     if ((s = launch_page_copies(ctx, kvs[0]->fp8, page_copies, st)) != RS_OK) return s;
+    rollback.armed = false;   // (the shared blocks that it continues have their copies)
     // 1/rms of every input row (the first RMSNorm; its gain lives in the packed W_qkv)
     tm.begin(RS_STEP_ROW_RMS);
     // and, in the same pass, x in the GEMMs' fragment-major token-operand layout

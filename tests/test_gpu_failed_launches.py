@@ -72,3 +72,19 @@ def test_an_append_that_fails_leaves_what_nobody_had_to_copy(apart):
         n = kv.length() - 3
         other.import_(0, torch.cat((k[:n], new[3 * i: 3 * i + 3])), torch.cat((v[:n], new[3 * i: 3 * i + 3])))
     assert torch.equal(out, ctx.attend(0, fresh, [3] * 5, q, torch.empty_like(q), ctx.attend_workspace(15, 5)))
+
+
+@pytest.mark.parametrize("kind", ["paged", "paged_fp8"])
+def test_a_prefill_that_cannot_copy_a_shared_block_changes_nothing(kind):
+    from tests.test_gpu_decode import rows, setup
+    from paper_2509_24381_amd import runner
+    dec, kvs, _, rng, stack = setup(kind)
+    fork = kvs[0].fork()
+    x = runner.to_device_bf16(rows(rng, 5, stack.shape.hidden))
+    held, shared, free = fork.length(), [fork.shared_pages(layer) for layer in range(2)], fork.pool.free_pages
+    assert held % 64 and min(shared) == (held + 63) // 64
+    fails(stack.ctx, lambda: stack.prefill_prompt(x, [(0, 5)], fork))
+    assert fork.length() == held and [fork.shared_pages(layer) for layer in range(2)] == shared and fork.pool.free_pages == free
+    y = stack.prefill_prompt(x, [(0, 5)], fork)
+    assert torch.equal(y, stack.prefill_prompt(x, [(0, 5)], kvs[0]))
+    assert [fork.shared_pages(layer) for layer in range(2)] == [s - 1 for s in shared]
