@@ -123,7 +123,7 @@ rs_status rs_weights_pack(rs_ctx* ctx, const rs_layer_weights* src, void* dst, s
  *   rs_kv_reset      all lengths := 0.
  *   rs_kv_truncate   length of `layer` := n_tokens (0 <= n_tokens <= current length): drops the newest tokens.
  *   rs_kv_export     copies the first rs_kv_len tokens to canonical bf16 [len][Hkv][d] arrays (post-RoPE K, V).
- *   rs_kv_import     loads n_tokens canonical rows as the cache content of `layer` and sets its length. */
+ *   rs_kv_import     loads n_tokens canonical rows as the cache content of `layer` and sets its length (RS_EHIP: `layer` is empty). */
 size_t rs_kv_bytes(const rs_ctx* ctx, int n_layers, int capacity_tokens);
 rs_status rs_kv_alloc(rs_ctx* ctx, int n_layers, int capacity_tokens, void* dev_mem, size_t bytes, rs_kv** out);
 void rs_kv_free(rs_kv* kv);

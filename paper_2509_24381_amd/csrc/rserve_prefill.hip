@@ -602,9 +602,14 @@ rs_status import_check(const rs_kv* kv, int layer, int n_tokens) {
     return RS_OK;
 }
 
+// Pages of its own for what arrives; until that has been enqueued the layer is empty.
+void start_import(rs_kv* kv, int layer, int n_tokens) {
+    if (kv->paged()) kv->replace_pages(layer, n_tokens);
+    kv->dropped_from(layer, 0);
+    kv->len[layer] = 0;
+}
 // The layer's content is new, and V behind it zero.
 void imported(rs_kv* kv, int layer, int n_tokens) {
-    kv->dropped_from(layer, 0);
     kv->len[layer] = n_tokens;
     kv->stale_tail[layer] = 0;
 }
@@ -1354,9 +1359,7 @@ rs_status rs_kv_import(rs_kv* kv, int layer, const void* k, const void* v, int n
     if (!k || !v) return fail(RS_EINVAL, "k / v is null");
     if (!kv->ctx->has_device) return fail(RS_EHIP, "no HIP device");
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    if (kv->paged()) {
-        kv->replace_pages(layer, n_tokens);
-    }
+    start_import(kv, layer, n_tokens);
     if (kv->fp8) {
         const rs_status s = fp8_import(kv, layer, (const bf16*)k, (const bf16*)v, n_tokens, st);
         if (s == RS_OK) imported(kv, layer, n_tokens);
@@ -1395,9 +1398,7 @@ rs_status rs_kv_import_codes(rs_kv* kv, int layer, const void* k_codes, const vo
     }
     if (!k_codes || !v_codes) return fail(RS_EINVAL, "k_codes / v_codes is null");
     if (!kv->ctx->has_device) return fail(RS_EHIP, "no HIP device");
-    if (kv->paged()) {
-        kv->replace_pages(layer, n_tokens);
-    }
+    start_import(kv, layer, n_tokens);
     const rs_status s = fp8_import(kv, layer, (const uint8_t*)k_codes, (const uint8_t*)v_codes, n_tokens, reinterpret_cast<hipStream_t>(stream));
     if (s == RS_OK) imported(kv, layer, n_tokens);
     return s;

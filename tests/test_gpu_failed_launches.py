@@ -88,3 +88,25 @@ def test_a_prefill_that_cannot_copy_a_shared_block_changes_nothing(kind):
     y = stack.prefill_prompt(x, [(0, 5)], fork)
     assert torch.equal(y, stack.prefill_prompt(x, [(0, 5)], kvs[0]))
     assert [fork.shared_pages(layer) for layer in range(2)] == [s - 1 for s in shared]
+
+
+@pytest.mark.parametrize("kind", ["contiguous", "paged", "paged_fp8"])
+@pytest.mark.parametrize("n", [20, 500])
+def test_an_import_that_fails_leaves_an_empty_cache(kind, n):
+    """Its pages are others than those that hold the tokens it had, or fewer."""
+    from paper_2509_24381_amd.binding import KVPool
+    ctx, g = context(4, 2, 64), gen(3)
+    pool = KVPool(ctx, 40, fp8=kind == "paged_fp8")
+    kv = ctx.kv_alloc(1, 512) if kind == "contiguous" else pool.new_cache(1)
+    old, new = normal(g, 300, 2, 64), normal(g, n, 2, 64)
+    kv.import_(0, old, old)
+    sharer = None if kind == "contiguous" else kv.fork()
+    fails(ctx, lambda: kv.import_(0, new, new))
+    assert kv.length() == 0 and kv.bounded(0) == 0
+    kv.import_(0, new, new)
+    fresh = ctx.kv_alloc_fp8(1, 512) if kind == "paged_fp8" else ctx.kv_alloc(1, 512)
+    for cache, x in ((kv, new), (sharer, old)):
+        if cache is None:
+            continue
+        fresh.import_(0, x, x)
+        assert all(torch.equal(*two) for two in zip(cache.export(0), fresh.export(0)))
