@@ -370,6 +370,15 @@ def _rows(t, what: str, rows: int, width: int):
     return t.data_ptr(), stride[0] if rows > 1 else width
 
 
+def _on_device(**tensors):
+    """Refuses tensors in host memory, whose addresses a kernel would follow.  (Hosts without a GPU: the call ends in the library's checks.)"""
+    for name, t in tensors.items():
+        if not t.is_cuda and t.numel() > 0:
+            import torch
+            if torch.cuda.is_available():
+                raise RsError(-1, f"{name} must be on the GPU: {t.device}")
+
+
 def _sum_of(a, n: int) -> int:
     return a[0] if n == 1 else sum(a[:n])
 
@@ -796,6 +805,7 @@ class Context:
         for t, dtype in zip(out, (torch.int32, torch.int32, torch.float32)):
             if t.dtype is not dtype or t.shape != (groups, n_select) or not t.is_contiguous():
                 raise RsError(-1, f"out must be contiguous int32, int32, fp32 [{groups}, {n_select}]: {t.dtype} {list(t.shape)}")
+        _on_device(logits=logits, scores=scores, workspace=workspace, parents=out[0], tokens=out[1], out_scores=out[2])
         _check(self.lib.rs_beam_select(self.handle, logits.data_ptr(), int(logits.dtype is torch.bfloat16), ld, shape[-1], groups, beams, scores.data_ptr(), n_select,
                                        out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_handle(stream)))
         return out
@@ -819,6 +829,7 @@ class Context:
         total = _sum_of(n, cs.n) if cs.n else 0
         if keep.dtype is not torch.int32 or not keep.is_contiguous() or keep.numel() != total:
             raise RsError(-1, f"keep must be contiguous int32 [{total}]: {keep.dtype} {list(keep.shape)}")
+        _on_device(keep=keep)
         _check(self.lib.rs_kv_compact(self.handle, layer, cs.handles, keep.data_ptr() if total else None, n, cs.n, _stream_handle(stream)))
         for i, kv in enumerate(cs.caches):
             kv.own_positions |= n[i] > 0
