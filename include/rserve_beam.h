@@ -43,7 +43,8 @@ extern "C" {
  *   logits     device, fp32 or bf16 (rs_logits_type), [n_groups * beams][vocab], rows ld_logits elements apart; no alignment but the elements'
  *   scores     device fp32 [n_groups * beams]; may be what out_scores was of a call before, not of this one
  *   workspace  256-byte aligned, rs_beam_workspace_bytes
- * 1 <= beams <= 64, 1 <= n_select <= 64, 1 <= vocab < 2^24, n_groups >= 0.  Unlike the calls that look at caches this one stages nothing on
+ * What is written, the workspace among it, overlaps neither logits or scores nor one another (RS_EINVAL).
+ * 1 <= beams <= 64, 1 <= n_select <= 64, 1 <= vocab < 2^24, n_groups >= 0, n_groups * beams <= 65535 (RS_EINVAL).  Unlike the calls that look at caches this one stages nothing on
  * the host and may be captured into a HIP graph. */
 typedef enum rs_logits_type { RS_LOGITS_F32 = 0, RS_LOGITS_BF16 = 1 } rs_logits_type;
 size_t rs_beam_workspace_bytes(const rs_ctx* ctx, int n_groups, int beams, int vocab);

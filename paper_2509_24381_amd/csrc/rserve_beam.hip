@@ -183,14 +183,19 @@ rs_status rs_beam_select(rs_ctx* ctx, const void* logits, int type, long ld_logi
     if (!aligned(logits, el) || !aligned(scores, 4) || !aligned(parents, 4) || !aligned(tokens, 4) || !aligned(out_scores, 4))
         return fail(RS_EINVAL, "logits, scores, parents, tokens and out_scores must be aligned to their elements");
     if (rows > 1 && ld_logits < vocab) return fail(RS_EINVAL, "ld_logits = %ld is smaller than a row (%d)", ld_logits, vocab);
-    // (a workgroup's results would be logits or scores that another has yet to read)
-    for (const void* p : {(const void*)parents, (const void*)tokens, (const void*)out_scores})
-        if (overlap(p, out, scores, rows * 4) || overlap(p, out, logits, ((rows - 1) * (size_t)ld_logits + vocab) * el))
-            return fail(RS_EINVAL, "parents, tokens and out_scores must not overlap logits or scores");
     const size_t need = rs_beam_workspace_bytes(ctx, n_groups, beams, vocab);
     if (!workspace) return fail(RS_EINVAL, "workspace is null");
     if (!aligned(workspace, 256)) return fail(RS_EINVAL, "workspace must be 256-byte aligned");
     if (workspace_bytes < need) return fail(RS_EWORKSPACE, "workspace has %zu bytes, this call needs %zu (rs_beam_workspace_bytes)", workspace_bytes, need);
+    // (a workgroup's results would be logits or scores that another has yet to read, or another's results)
+    const std::pair<const void*, size_t> written[] = {{parents, out}, {tokens, out}, {out_scores, out}, {workspace, need}};
+    for (const auto& x : written) {
+        if (overlap(x.first, x.second, scores, rows * 4) || overlap(x.first, x.second, logits, ((rows - 1) * (size_t)ld_logits + vocab) * el))
+            return fail(RS_EINVAL, "parents, tokens, out_scores and workspace must not overlap logits or scores");
+        for (const auto& y : written)
+            if (&x != &y && overlap(x.first, x.second, y.first, y.second))
+                return fail(RS_EINVAL, "parents, tokens, out_scores and workspace must not overlap one another");
+    }
     if ((s = check_device(ctx)) != RS_OK) return s;
     BeamArgs a{};
     a.logits = logits; a.ld = ld_logits; a.vocab = vocab; a.beams = beams; a.n_select = n_select;
