@@ -15,6 +15,8 @@ from typing import List, Optional, Sequence
 from .binding import CacheSet, Context, KVCache, RotaryConfig, RsError, int_array
 from .runner import to_device_bf16
 
+BEAMS = 64   # of a group, and continuations of one, that rs_beam_select takes
+
 
 class _Layer:
     """One layer's parameters in torch layout, bf16 on the device."""
@@ -133,8 +135,12 @@ class Decoder:
         """The best continuations of every request's prompt that a search over `beams` beams finds: lists of (tokens, score), best first, score the sum
         of the tokens' log-probabilities over the number of tokens to the power length_power.  A continuation ends with token `end` (which is
         among its tokens), or after n_tokens.  kvs: paged caches, which stay as they are; the pools need pages for the beams' own tokens, max_rows
-        and max_requests to be the requests times the beams.  last_rows, embedding, final_gain, w_lm, positions: as for greedy."""
+        and max_requests to be the requests times the beams.  n_tokens >= 1, 1 <= beams <= 64, with `end` 32.  last_rows, embedding, final_gain, w_lm,
+        positions: as for greedy."""
         import torch
+        most = BEAMS if end is None else BEAMS // 2   # (twice as many are selected)
+        if n_tokens < 1 or not 1 <= beams <= most:
+            raise RsError(-1, f"a beam search takes n_tokens >= 1 and 1 <= beams <= {most}: {n_tokens}, {beams}")
         prompts = kvs.caches if isinstance(kvs, CacheSet) else list(kvs)
         requests, n_select = len(prompts), beams if end is None else 2 * beams   # (of a beam one continuation at most ends)
         held = [kv.length(0) for kv in prompts]
