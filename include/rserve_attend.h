@@ -95,7 +95,8 @@ rs_status rs_kv_append(rs_ctx* ctx, const rs_rotary* rotary, int layer, rs_kv* c
  * that they see to bfloat16 in the workspace first.  A code is exact there, and the scales enter the softmax's scale and the output, so
  * that either way a key or value is code * scale (rs_prefill_* round that to bfloat16).
  * Requests next to each other whose caches start with the same pages (rs_kv_fork, rserve_beam.h) have these read once for all of them, where that is
- * enough to pay; a row's bits then depend on its neighbours, within the same rounding.
+ * enough to pay, all of the call's caches are on one pool with the same scales, max_tokens_per_call is at most 65535 and max_pos at most 4000000; a row's bits then
+ * depend on its neighbours, within the same rounding.  Else every request reads its cache alone.
  * TEST-ONLY environment variables read in rs_ctx_create: RS_ATTEND_FEW=n replaces the size up to which "more rows" are few (0: never),
  * RS_ATTEND_SHARE=n the bytes that sharing has to leave unread (0: none), RS_ATTEND_TOGETHER=n the tiles from which fewer rows share them in a workgroup (0: always).
  *   workspace   256-byte aligned, rs_attend_workspace_bytes:
