@@ -805,7 +805,8 @@ class Context:
         for t, dtype in zip(out, (torch.int32, torch.int32, torch.float32)):
             if t.dtype is not dtype or t.shape != (groups, n_select) or not t.is_contiguous():
                 raise RsError(-1, f"out must be contiguous int32, int32, fp32 [{groups}, {n_select}]: {t.dtype} {list(t.shape)}")
-        _on_device(logits=logits, scores=scores, workspace=workspace, parents=out[0], tokens=out[1], out_scores=out[2])
+        if not (logits.is_cuda and scores.is_cuda and workspace.is_cuda and out[0].is_cuda and out[1].is_cuda and out[2].is_cuda):
+            _on_device(logits=logits, scores=scores, workspace=workspace, parents=out[0], tokens=out[1], out_scores=out[2])
         _check(self.lib.rs_beam_select(self.handle, logits.data_ptr(), int(logits.dtype is torch.bfloat16), ld, shape[-1], groups, beams, scores.data_ptr(), n_select,
                                        out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_handle(stream)))
         return out
@@ -829,7 +830,8 @@ class Context:
         total = _sum_of(n, cs.n) if cs.n else 0
         if keep.dtype is not torch.int32 or not keep.is_contiguous() or keep.numel() != total:
             raise RsError(-1, f"keep must be contiguous int32 [{total}]: {keep.dtype} {list(keep.shape)}")
-        _on_device(keep=keep)
+        if not keep.is_cuda:
+            _on_device(keep=keep)
         _check(self.lib.rs_kv_compact(self.handle, layer, cs.handles, keep.data_ptr() if total else None, n, cs.n, _stream_handle(stream)))
         for i, kv in enumerate(cs.caches):
             kv.own_positions |= n[i] > 0
