@@ -41,8 +41,8 @@ inline size_t fewest_slots(const std::vector<FewRequest>& reqs) {
 // 13.0 / 13.8, 1 on 32000 (2000) 22.9 / 25.8, 16 on 8000 (4520) 51.4 / 43.5, 8 bits 34.7 / 32.7; 8 beams, 8 on 8000 (2130) 37.7 / 32.0.
 constexpr long TOGETHER_TILES = 3000;
 // That takes more slots: 17 to 32 rows are two blocks of 16 apart and eight together, more rows up to twice as many.  So those of up to 32 rows are only
-// together if all sums have room then (51 prompts with 3 beams, (h): 4488 of 4096 slots together, 2040 apart), and share_pages leaves twice the slots that are
-// taken apart.  Sets units and row_blocks of those that are together; returns FewShared::together.
+// together if all sums have room then (51 prompts with 3 beams, (h): 4488 of 4096 slots together, 2040 apart; on 4000 209 us a pass apart, 331 with each request
+// alone), and share_pages leaves twice the slots that are taken apart.  Sets units and row_blocks of those that are together; returns FewShared::together.
 inline int share_tiles(std::vector<FewRequest>& reqs, int g, int hkv, long from, size_t slots) {
     long tiles = 0;
     for (const FewRequest& r : reqs)
