@@ -241,6 +241,29 @@ __attribute__((visibility("hidden"))) rs_status launch_page_copies(const rs_ctx*
 // ring_commit ends the use, behind the last kernel that reads the slot.
 __attribute__((visibility("hidden"))) rs_status ring_acquire(rs_ctx* ctx, hipStream_t st, int* slot);
 __attribute__((visibility("hidden"))) rs_status ring_commit(rs_ctx* ctx, hipStream_t st);
+// A call's use of it, which ends with the call at the latest: one that returns an error may have launched what reads the slot.
+class RingUse {
+    rs_ctx* const ctx;
+    const hipStream_t st;
+    bool open = false;
+
+public:
+    RingUse(rs_ctx* c, hipStream_t stream) : ctx(c), st(stream) {}
+    RingUse(const RingUse&) = delete;
+    RingUse& operator=(const RingUse&) = delete;
+    ~RingUse() {
+        if (open) (void)ring_commit(ctx, st);
+    }
+    rs_status acquire(int* slot) {
+        const rs_status s = ring_acquire(ctx, st, slot);
+        open = s == RS_OK;
+        return s;
+    }
+    rs_status commit() {
+        open = false;
+        return ring_commit(ctx, st);
+    }
+};
 
 // RS_ESTATE if `st` is capturing a HIP graph (a replay would find stale descriptors).
 __attribute__((visibility("hidden"))) rs_status refuse_capture(hipStream_t st);

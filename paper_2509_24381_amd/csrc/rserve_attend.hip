@@ -711,7 +711,8 @@ rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, 
     }
     const bool staged = chunks || few_staged != NOTHING;
     int slot = 0;
-    if (staged && (s = ring_acquire(ctx, st, &slot)) != RS_OK) return s;
+    RingUse ring(ctx, st);
+    if (staged && (s = ring.acquire(&slot)) != RS_OK) return s;
     char* const stage = staged ? ctx->pinned[slot] : nullptr;
     size_t staged_bytes = 0;
     if (few_staged == ALL) {
@@ -793,7 +794,7 @@ rs_status rs_attend(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int* lens, 
         else with_table(tab, few_words + (few_staged == NOTHING ? few_pages : 0), launch);
         if (s != RS_OK) return s;
     }
-    if (staged && (s = ring_commit(ctx, st)) != RS_OK) return s;
+    if (staged && (s = ring.commit()) != RS_OK) return s;
     if (!chunks) return RS_OK;
     const ReqDesc* const d_reqs = reinterpret_cast<const ReqDesc*>(ws + at_reqs);
     const AttnItem* const d_items = reinterpret_cast<const AttnItem*>(ws + at_items);
@@ -941,7 +942,8 @@ rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int*
                           (split == 1 || fits || longest <= SELECTED_IN_PLACE_BLOCKS || units >= SELECTED_IN_PLACE_UNITS);
     const bool in_arguments = selected && fits;
     int slot = 0;
-    if (!in_arguments && (s = ring_acquire(ctx, st, &slot)) != RS_OK) return s;
+    RingUse ring(ctx, st);
+    if (!in_arguments && (s = ring.acquire(&slot)) != RS_OK) return s;
     uint32_t* const stage = in_arguments ? nullptr : reinterpret_cast<uint32_t*>(ctx->pinned[slot]);
 
     SelectArgs sa{};
@@ -1018,7 +1020,7 @@ rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int*
             });
         });
         RS_HIP(hipGetLastError());
-        return in_arguments ? RS_OK : ring_commit(ctx, st);
+        return in_arguments ? RS_OK : ring.commit();
     }
     // the attention kernel's table, copied by the first selection launch
     write_few_table(ctx, layer, kvs, reqs, true, false, stage, stage + few_words);
@@ -1052,7 +1054,7 @@ rs_status rs_attend_blocks(rs_ctx* ctx, int layer, rs_kv* const* kvs, const int*
         if (f.head_dim == 128) select(std::integral_constant<int, 128>{});
         else select(std::integral_constant<int, 64>{});
         RS_HIP(hipGetLastError());
-        if (i0 == 0 && (s = ring_commit(ctx, st)) != RS_OK) return s;
+        if (i0 == 0 && (s = ring.commit()) != RS_OK) return s;
     }
     a.table = reinterpret_cast<const uint32_t*>(ws);
     a.chosen = sa.chosen;

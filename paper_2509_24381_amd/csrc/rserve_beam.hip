@@ -41,7 +41,8 @@ rs_status launch_moves(rs_ctx* ctx, bool fp8, const std::vector<Move>& moves, co
         InlineTable tab;
         int slot = 0;
         rs_status s;
-        if (!inside && (s = ring_acquire(ctx, st, &slot)) != RS_OK) return s;
+        RingUse ring(ctx, st);
+        if (!inside && (s = ring.acquire(&slot)) != RS_OK) return s;
         uint32_t* const numbers = inside ? tab.w + words : reinterpret_cast<uint32_t*>(ctx->pinned[slot]);
         MoveArgs a{};
         a.n_req = n;
@@ -87,9 +88,8 @@ rs_status launch_moves(rs_ctx* ctx, bool fp8, const std::vector<Move>& moves, co
                 else hipLaunchKernelGGL((kv_copy_kernel<D, FP8, Tab>), dim3(items, 2u * a.hkv * CopyPiece<D, FP8>::PIECES), dim3(256), 0, st, a, table);
             });
         });
-        const hipError_t launched = hipGetLastError();
-        if (!inside && (s = ring_commit(ctx, st)) != RS_OK) return s;   // (whatever has failed: page numbers may be read all the same)
-        RS_HIP(launched);
+        RS_HIP(hipGetLastError());
+        if (!inside && (s = ring.commit()) != RS_OK) return s;
         i0 = i1;
     }
     return RS_OK;

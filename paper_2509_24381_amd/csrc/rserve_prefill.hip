@@ -835,7 +835,8 @@ rs_status prefill_enqueue(rs_ctx* ctx, const rs_layer_weights* w, int layer, rs_
 
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     int slot = 0;
-    rs_status s = ring_acquire(ctx, st, &slot);
+    RingUse ring(ctx, st);
+    rs_status s = ring.acquire(&slot);
     if (s != RS_OK) return s;
     char* stage = ctx->pinned[slot];
     memcpy(stage, reqs.data(), sizeof(ReqDesc) * reqs.size());
@@ -902,7 +903,7 @@ rs_status prefill_enqueue(rs_ctx* ctx, const rs_layer_weights* w, int layer, rs_
     else if (red.splits > MAX_PLANES) first_kernel(std::integral_constant<int, MAX_PLANES_FEW>{}, std::integral_constant<int, 256>{});
     else first_kernel_lanes(std::integral_constant<int, MAX_PLANES>{});
     RS_HIP(hipGetLastError());
-    if ((s = ring_commit(ctx, st)) != RS_OK) return s;
+    if ((s = ring.commit()) != RS_OK) return s;
     tm.end(RS_STEP_ROW_RMS);
     // qkv = rope( (x Wqkv'^T) / rms + b )
     tm.begin(RS_STEP_QKV_GEMM);

@@ -110,3 +110,42 @@ def test_an_import_that_fails_leaves_an_empty_cache(kind, n):
             continue
         fresh.import_(0, x, x)
         assert all(torch.equal(*two) for two in zip(cache.export(0), fresh.export(0)))
+
+
+@pytest.mark.parametrize("blocks", [0, 8])
+def test_page_numbers_of_a_call_that_fails_stay_until_they_are_read(blocks):
+    """The calls behind it stage theirs elsewhere: the kernel of a call that reports an error reads its own."""
+    from paper_2509_24381_amd.binding import KVPool, RsError
+    ctx, g = context(4, 2, 64), gen(4)
+    pool = KVPool(ctx, 4 * 600)
+    kvs = [pool.new_cache(1) for _ in range(4)]
+    for kv in kvs:
+        k, v = normal(g, 38000, 2, 64), normal(g, 38000, 2, 64)
+        kv.import_(0, k, v)
+        if blocks:
+            kv.new_bounds(38400)
+    q = normal(g, 2, 4 * 64)
+
+    def attend(pair, out):
+        ws = ctx.attend_workspace(2, 2, n_blocks=blocks)
+        return lambda: ctx.attend_blocks(0, pair, [1, 1], q, out, ws, blocks) if blocks else ctx.attend(0, pair, [1, 1], q, out, ws)
+
+    out = [torch.zeros_like(q) for _ in range(20)]
+    calls = [attend(kvs[i % 2 * 2: i % 2 * 2 + 2], o) for i, o in enumerate(out)]
+    want = []
+    for call, o in zip(calls[:2], out):
+        call()
+        want.append(o.clone())
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for i, call in enumerate(calls):
+            out[i].zero_()
+            if i % 3 == 0:
+                assert ctx.lib.hipSetDevice(1 << 20) != 0
+                with pytest.raises(RsError, match="invalid device"):
+                    call()
+                ctx.lib.hipGetLastError()
+            else:
+                call()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, want[i % 2]) for i, o in enumerate(out) if i % 3 or not blocks)   # (blocks: a launch that follows is left out)
